@@ -1,0 +1,151 @@
+// Passes over 8-bit rows (q8_common.hpp): values -> rows, layernorm + modulate -> rows, rows -> values with the gated residual.
+// Each touches every element once: they are bound by HBM.
+#pragma once
+#include "module_rowwise.hpp"
+#include "q8_common.hpp"
+
+namespace pab {
+
+struct QuantizeParams {
+  const void *x;            // [rows, K], row pitch ldx elements
+  unsigned char *data, *scale;
+  long long ldx, ld, ld_scale;
+  int K;
+  unsigned n_item;          // rows * blocks per row
+  Divisor nb;               // blocks per row
+};
+
+// 16 lanes take a block of 128 values, 8 each.
+template <typename T>
+__global__ __launch_bounds__(256) void quantize_kernel(const QuantizeParams p) {
+  const unsigned item = blockIdx.x * 16 + (threadIdx.x >> 4);
+  const int part = threadIdx.x & 15;
+  const bool live = item < p.n_item;
+  const unsigned row = quotient(live ? item : 0, p.nb), b = (live ? item : 0) - row * p.nb.d;
+  const int c = 128 * (int)b + 8 * part;
+  float v[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+  if (live && c < p.K) load_row8(static_cast<const T *>(p.x) + row * p.ldx + c, v);
+  unsigned big = 0;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) big = max(big, finite_bits(v[e]));
+  const int byte = q8_scale_byte(max16(big));
+  const float inv = q8_inverse(byte);
+#pragma unroll
+  for (int e = 0; e < 8; ++e) v[e] = q8_scaled(v[e], inv);
+  if (!live) return;
+  *reinterpret_cast<u32x2 *>(p.data + row * p.ld + c) = u32x2{pack_e4m3(v[0], v[1], v[2], v[3]), pack_e4m3(v[4], v[5], v[6], v[7])};
+  if (part == 0) p.scale[row * p.ld_scale + b] = (unsigned char)byte;
+}
+
+struct DequantizeParams {
+  const unsigned char *data, *scale;
+  const void *x;            // [rows, K] or nullptr: out = x + gate * value
+  const void *gate;         // [K] or nullptr: 1
+  void *out;
+  long long ld, ld_scale, ldx, ldo;
+  int K;
+  unsigned n_item;          // rows * chunks of 8 columns
+  Divisor nc;               // chunks per row
+};
+
+// A lane takes 8 columns.
+template <typename T>
+__global__ __launch_bounds__(256) void dequantize_kernel(const DequantizeParams p) {
+  const unsigned item = blockIdx.x * 256 + threadIdx.x;
+  if (item >= p.n_item) return;
+  const unsigned row = quotient(item, p.nc);
+  const int c = 8 * (int)(item - row * p.nc.d);
+  const u32x2 d = *reinterpret_cast<const u32x2 *>(p.data + row * p.ld + c);
+  const float s = q8_scale(p.scale[row * p.ld_scale + (c >> 7)]);
+  float v[8];
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)d[h], false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)d[h], true);
+    v[4 * h] = lo[0] * s; v[4 * h + 1] = lo[1] * s; v[4 * h + 2] = hi[0] * s; v[4 * h + 3] = hi[1] * s;
+  }
+  if (p.gate) {
+    float g[8];
+    load_row8(static_cast<const T *>(p.gate) + c, g);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] *= g[e];
+  }
+  if (p.x) {
+    float x[8];
+    load_row8(static_cast<const T *>(p.x) + row * p.ldx + c, x);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] += x[e];
+  }
+  store_row8(static_cast<T *>(p.out) + row * p.ldo + c, v);
+}
+
+struct LnQ8Params {
+  const bf16_t *x, *shift, *scale;   // [n_tok, C], [C], [C]
+  unsigned char *data, *scales;
+  long long ld, ld_scale;
+  int n_tok, C;
+  float eps;
+};
+
+// ln_modulate_kernel (module_rowwise.hpp) that leaves 8-bit rows: a lane's chunks of 8 columns are 64 apart, so 16 neighbouring lanes
+// hold a block of 128.  The normed row is quantised from fp32, without the rounding to bf16 in between.
+template <int NCH>
+__global__ __launch_bounds__(256) void ln_modulate_q8_kernel(const LnQ8Params p) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int tok = blockIdx.x * 4 + wave;
+  if (tok >= p.n_tok) return;
+  const int C = p.C, nchunk = C >> 3, npad = (C + 127) / 128 * 16;
+  const bf16_t *xr = p.x + (long long)tok * C;
+  bf16x8 x[NCH], sh[NCH], sc[NCH];
+#pragma unroll
+  for (int i = 0; i < NCH; ++i) x[i] = lane + 64 * i < nchunk ? *reinterpret_cast<const bf16x8 *>(xr + 8 * (lane + 64 * i)) : zero8();
+#pragma unroll
+  for (int i = 0; i < NCH; ++i) {
+    sh[i] = sc[i] = zero8();
+    if (lane + 64 * i < nchunk) {
+      sh[i] = *reinterpret_cast<const bf16x8 *>(p.shift + 8 * (lane + 64 * i));
+      sc[i] = *reinterpret_cast<const bf16x8 *>(p.scale + 8 * (lane + 64 * i));
+    }
+  }
+  float v[NCH][8];
+  float s = 0.0f;
+#pragma unroll
+  for (int i = 0; i < NCH; ++i)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      v[i][e] = (float)x[i][e];
+      s += v[i][e];
+    }
+  const float mean = wave_sum(s) / (float)C;
+  float ss = 0.0f;
+#pragma unroll
+  for (int i = 0; i < NCH; ++i)
+    if (lane + 64 * i < nchunk) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float d = v[i][e] - mean;
+        ss += d * d;
+      }
+    }
+  const float rstd = 1.0f / sqrtf(wave_sum(ss) / (float)C + p.eps);
+#pragma unroll
+  for (int i = 0; i < NCH; ++i) {
+    const int c = lane + 64 * i;
+    float y[8];
+    unsigned big = 0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      y[e] = c < nchunk ? (v[i][e] - mean) * rstd * (1.0f + (float)sc[i][e]) + (float)sh[i][e] : 0.0f;
+      big = max(big, finite_bits(y[e]));
+    }
+    const int byte = q8_scale_byte(max16(big));
+    const float inv = q8_inverse(byte);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) y[e] = q8_scaled(y[e], inv);
+    if (c < npad) {
+      *reinterpret_cast<u32x2 *>(p.data + tok * p.ld + 8 * c) = u32x2{pack_e4m3(y[0], y[1], y[2], y[3]), pack_e4m3(y[4], y[5], y[6], y[7])};
+      if ((lane & 15) == 0) p.scales[tok * p.ld_scale + (c >> 4)] = (unsigned char)byte;
+    }
+  }
+}
+
+}  // namespace pab

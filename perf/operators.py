@@ -196,12 +196,12 @@ def _run_own(s):
         return pab.pab_dequantize(pab.Q8(s["data"], s["scale"], case["K"]), s.get("x"), s.get("gate"), dtype=FLOAT[case["dtype"]])
     if form == "linear":
         a, w = pab.Q8(*s["a"], case["K"]), pab.Q8(*s["w"], case["K"])
-        return pab.pab_linear_q8(a, w, s["bias"], act=pab.GELU if case["act"] == "gelu" else pab.NONE)
+        return pab.pab_linear_quantized(a, w, s["bias"], act=pab.GELU if case["act"] == "gelu" else pab.NONE)
     if form == "qk":
         norm = {"none": pab.NORM_NONE, "layer": pab.NORM_LAYER, "rms": pab.NORM_RMS}[case["norm"]]
         return pab.pab_qk_norm_rope(s["q"], s["k"], (case["T"], case["Y"], case["X"]), s["axes"], s["factors"], norm, *s["weights"], eps=1e-6)
-    w = pab.mlp_weights_q8(s["shift"], s["mod"], pab.Q8(*s["w1"], case["hidden"]), s["b1"], pab.Q8(*s["w2"], case["inner"]), s["b2"])
-    return pab.pab_mlp_compute_q8(s["x"], w)
+    w = pab.mlp_weights_quantized(s["shift"], s["mod"], pab.Q8(*s["w1"], case["hidden"]), s["b1"], pab.Q8(*s["w2"], case["inner"]), s["b2"])
+    return pab.pab_mlp_compute_quantized(s["x"], w)
 
 
 def _norm(v, norm, gamma, beta, eps):
