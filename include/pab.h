@@ -367,6 +367,157 @@ long long pab_mlp_launch_count(const pab_mlp_ctx *ctx);
 const void *pab_mlp_slot_ptr(const pab_mlp_ctx *ctx, int block);
 int pab_mlp_destroy(pab_mlp_ctx *ctx);
 
+/*
+ * 8-bit rows.  The operations below keep matrices in e4m3 (4 exponent bits, 3
+ * mantissa bits, largest value 448, no infinities) with a scale for each block
+ * of 128 columns of a row.  A matrix [rows, K] is
+ *   data:  bytes, row pitch `ld`; a row holds K values and zeros up to the next
+ *          multiple of 128 columns.  16-byte aligned, ld a multiple of 16.
+ *   scale: exponent bytes, row pitch `ld_scale`; byte b of block c stands for
+ *          2^(b - 127) (255: NaN).  4-byte aligned, ld_scale a multiple of 4
+ *          and at least ceil(K / 128) rounded up to one; the bytes behind the
+ *          last block have no meaning.
+ * An element is its e4m3 value times its block's scale.  Both pitches are at
+ * most 2^24.  The struct is host memory, read (and, where said, written) during
+ * the call only; data and scale are the caller's device memory.
+ *
+ * How values become 8-bit rows, everywhere below: the scale of a block is the
+ * smallest power of two, 2^-127 at least, for which its largest finite
+ * magnitude stays within 448; values are divided by it and rounded to nearest,
+ * ties to even, once from fp32.  An error is therefore at most 2^-4 of the value,
+ * or 2^-10 of the scale where the value is below 2^-6 of it.  Infinities and
+ * NaNs become NaN and do not count for the scale.
+ */
+typedef struct pab_q8 {
+  void *data, *scale;
+  long long ld, ld_scale;
+} pab_q8;
+
+/* Bytes of one buffer that holds 8-bit rows [rows, K] densely (data, then scales, each rounded up to 256 bytes; 0:
+ * rows or K < 1 or too large), and the matrix in such a buffer (host, pure).  PAB_EINVAL: NULL, buffer not 256-byte
+ * aligned.  PAB_ENOMEM: buffer too small. */
+size_t pab_quantized_bytes(long long rows, int K);
+int pab_quantized_layout(long long rows, int K, void *buffer, size_t bytes, pab_q8 *out);
+
+/*
+ * Values to 8-bit rows: x [rows, K] of type dtype, row pitch ldx elements, ->
+ * y, padding columns included.  One launch on `hip_stream`.
+ * PAB_EINVAL: rows < 1, K not a positive multiple of 8, a pitch that is too
+ * small or no multiple of 16 bytes, NULL or misaligned pointers, unknown dtype,
+ * more than 2^28 blocks.  PAB_EDEVICE: launch failed.
+ */
+int pab_quantize(long long rows, int K, int dtype, const void *x, long long ldx, const pab_q8 *y, void *hip_stream);
+
+/*
+ * 8-bit rows to values, added to a residual stream: out = x + gate * y, with x
+ * [rows, K] (row pitch ldx) or NULL for 0 and gate [K] or NULL for 1, all of
+ * type dtype; computed in fp32 and rounded once.  out may be x.  One launch.
+ * Errors as pab_quantize.
+ */
+int pab_dequantize(long long rows, int K, int dtype, const pab_q8 *y, const void *x, long long ldx, const void *gate, void *out,
+                   long long ldo, void *hip_stream);
+
+/*
+ * pab_linear on 8-bit rows: C = act(A W^T + bias).  A: 8-bit rows [M, K], W:
+ * 8-bit rows [N, K], bias: bf16 [N] or NULL; act: none or GELU in its tanh
+ * form.  Products of e4m3 values times their scales are added by the matrix
+ * core: eight neighbouring columns at a time, lined up to the largest product
+ * and cut 13 binary places below it, and these sums in fp32.  The output is bf16 C [M, N] with a row pitch of ldc elements, rounded once, or
+ * 8-bit rows C8 [M, N] (quantised from the fp32 sums); exactly one of the two
+ * is given.  C and C8 must not overlap A or W.  One launch on `hip_stream`.
+ * PAB_EINVAL: M < 1, N or K not a positive multiple of 8, unknown act, both or
+ * neither output, NULL or misaligned pointers, bad pitches.
+ * Sums below the smallest normal fp32 number may be lost.
+ */
+enum pab_activation { PAB_NONE = 0, PAB_GELU = 1 };
+int pab_linear_quantized(int M, int N, int K, const pab_q8 *A, const pab_q8 *W, const void *bias, int act, void *C, long long ldc,
+                         const pab_q8 *C8, void *hip_stream);
+
+/*
+ * The MLP module on 8-bit rows: pab_mlp_compute with both products through
+ * pab_linear_quantized; what stands between them is quantised from fp32 inside
+ * the kernels that produce it.  x, out, shift, scale, b1, b2 as there; w1
+ * [inner, hidden], w2 [hidden, inner] are 8-bit rows (pab_quantize of the
+ * weights, once).  Three launches.  Errors as pab_mlp_compute, at most 2^25
+ * tokens.
+ */
+typedef struct pab_mlp_weights_quantized {
+  const void *shift, *scale;
+  pab_q8 w1;
+  const void *b1;
+  pab_q8 w2;
+  const void *b2;
+} pab_mlp_weights_quantized;
+size_t pab_mlp_scratch_bytes_quantized(long long n_tok, int hidden, int inner);
+int pab_mlp_compute_quantized(long long n_tok, int hidden, int inner, const void *x, const pab_mlp_weights_quantized *w, void *scratch,
+                              size_t scratch_bytes, void *out, void *hip_stream);
+
+/*
+ * A broadcast cache of 8-bit rows: half the bytes of a bf16 cache, a quarter of
+ * an fp32 one.  A context made by pab_create_quantized has the schedule, errors
+ * and life of one made by pab_create (pab_reset, pab_launch_count, pab_slot_ptr
+ * (the slot's data) and pab_destroy take it), but a slot holds 8-bit rows
+ * [T * S, heads * head_dim], and it is used through the calls below; the calls
+ * for one sort of context refuse the other (PAB_EINVAL).  On a computed step
+ * the attention or the module runs and its output is quantised into the slot
+ * (one launch more); on a reused step nothing is launched or read.  *out
+ * receives the slot as a borrowed, read-only matrix for pab_dequantize or, as
+ * its operand A, pab_linear_quantized.
+ * scratch: pab_attention_quantized needs the bytes of one output tensor [T, S,
+ * heads, head_dim] (16-byte aligned), pab_module_attention_quantized those of
+ * pab_module_attention; needed on computed steps only.
+ */
+size_t pab_workspace_bytes_quantized(const pab_config *cfg);
+int pab_create_quantized(const pab_config *cfg, void *workspace, size_t workspace_bytes, pab_ctx **out);
+int pab_attention_quantized(pab_ctx *ctx, int block, int kind, int step, const void *q, const void *k, const void *v, void *scratch,
+                            size_t scratch_bytes, void *hip_stream, pab_q8 *out);
+int pab_module_attention_quantized(pab_ctx *ctx, int block, int kind, int step, const void *x, const void *text,
+                                   const pab_module_weights *w, void *scratch, size_t scratch_bytes, void *hip_stream, pab_q8 *out);
+/* The slot without touching any state. PAB_EINVAL: not such a context, no such slot. */
+int pab_slot_quantized(const pab_ctx *ctx, int block, int kind, pab_q8 *out);
+
+/*
+ * Norm of queries and keys per head and rotation over up to three axes (frame,
+ * row, column), in one pass, for models that attend over the whole clip or
+ * place their tokens in a frame.  Tokens are n_batch grids of places[0] x
+ * places[1] x places[2] in that order, the last axis fastest; a token's
+ * queries are [heads_q, head_dim] and its keys [heads_k, head_dim], dense,
+ * tokens ld_* elements apart (so q and k may be parts of one buffer).
+ *   y = LayerNorm(x) * gamma + beta | x / sqrt(mean(x^2) + eps) * gamma + beta | x * gamma + beta
+ * over the head dimension, biased variance; gamma, beta [head_dim], NULL = 1, 0.
+ * Then the first axis_dim[0] features of a head are turned by the place on axis
+ * 0, the next axis_dim[1] by that on axis 1, and so on; what is left is not
+ * turned.  Pairs (2i, 2i+1) of a section turn by the angle of pair i, whose
+ * (cos, sin) are read from `factors`: fp32 pairs, axis by axis, place by place,
+ * pair by pair, pab_rope_factors_count of them (NULL: no rotation).  fp32
+ * arithmetic, rounded once.  The outputs may be the inputs (same pointer and
+ * pitch), otherwise they must not overlap them.  heads_k = 0: queries only.
+ * head_dim 32, 64, 72, 96 or 128; at most 2^27 (token, head) rows.  One launch.
+ */
+enum pab_norm { PAB_NORM_NONE = 0, PAB_NORM_LAYER = 1, PAB_NORM_RMS = 2 };
+typedef struct pab_qk_norm {
+  int dtype, norm, n_batch, heads_q, heads_k, head_dim;
+  int places[3], axis_dim[3];
+  float eps;
+  const void *q, *k;
+  void *q_out, *k_out;
+  long long ld_q, ld_k, ld_q_out, ld_k_out;
+  const void *gamma_q, *beta_q, *gamma_k, *beta_k;
+  const void *factors;
+} pab_qk_norm;
+int pab_qk_norm_rope(const pab_qk_norm *d, void *hip_stream);
+
+/*
+ * The table of pab_qk_norm_rope: (cos, sin) of (origin[a] + place * step[a]) *
+ * theta^(-2i / axis_dim[a]), computed in fp64 and rounded once.  origin NULL: 0,
+ * step NULL: 1 (others: a part of a clip, positions stretched from another
+ * resolution).  pab_rope_factors_count is the number of pairs (8 bytes each),
+ * or PAB_EINVAL: a place count < 1, an axis_dim odd or negative, too many.
+ */
+long long pab_rope_factors_count(const int places[3], const int axis_dim[3]);
+int pab_rope_factors(const int places[3], const int axis_dim[3], const double origin[3], const double step[3], double theta,
+                     void *factors, void *hip_stream);
+
 /* Computed calls issued through ctx since pab_create / the last pab_reset: one
  * per call of pab_attention / pab_module_attention that the schedule decided
  * to compute (an operation-level call is one kernel launch, a module-level

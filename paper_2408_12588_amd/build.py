@@ -14,6 +14,8 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libpab.so")
 SOURCES = [os.path.join(CSRC, "pab_api.hip")]
+# built without -fno-honor-nans: the quantisers of 8-bit rows look for NaNs
+SOURCES_NAN = [os.path.join(CSRC, "q8_api.hip")]
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",
     # packed fp32 VALU forms stay off for device code (the host pass does not know the
@@ -31,16 +33,34 @@ HIPCC_FLAGS = [
 def build_lib(verbose: bool = False, extra_flags=()) -> str:
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
     tmp = LIB + ".tmp.%d" % os.getpid()
-    cmd = [hipcc] + HIPCC_FLAGS + list(extra_flags) + ["-o", tmp] + SOURCES
-    if verbose:
-        print(" ".join(cmd), flush=True)
-    res = subprocess.run(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
-    out = "\n".join(l for l in res.stdout.splitlines() if "packed-fp32-ops" not in l)
-    if res.returncode != 0:
-        sys.stderr.write(out + "\n")
-        raise RuntimeError("hipcc failed building libpab.so")
-    if verbose and out.strip():
-        print(out)
+    jobs, objects = [], []
+    for sources, flags in ((SOURCES, HIPCC_FLAGS), (SOURCES_NAN, [f for f in HIPCC_FLAGS if f != "-fno-honor-nans"])):
+        for src in sources:
+            objects.append("%s.%s.o" % (tmp, os.path.basename(src)))
+            cmd = [hipcc] + [f for f in flags if f != "-shared"] + list(extra_flags) + ["-c", "-o", objects[-1], src]
+            if verbose:
+                print(" ".join(cmd), flush=True)
+            jobs.append((cmd, subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)))
+    failed = False
+    for cmd, job in jobs:
+        out = "\n".join(l for l in job.communicate()[0].splitlines() if "packed-fp32-ops" not in l)
+        if job.returncode != 0:
+            sys.stderr.write(out + "\n")
+            failed = True
+        elif verbose and out.strip():
+            print(out)
+    try:
+        if failed:
+            raise RuntimeError("hipcc failed building libpab.so")
+        res = subprocess.run([hipcc, "--offload-arch=gfx950", "-shared", "-o", tmp] + objects, stdout=subprocess.PIPE,
+                             stderr=subprocess.STDOUT, text=True)
+        if res.returncode != 0:
+            sys.stderr.write(res.stdout + "\n")
+            raise RuntimeError("hipcc failed linking libpab.so")
+    finally:
+        for o in objects:
+            if os.path.exists(o):
+                os.unlink(o)
     os.replace(tmp, LIB)
     return LIB
 

@@ -44,12 +44,13 @@ __device__ __forceinline__ f32x4 mfma_q8(i32x8 w, i32x8 t, f32x4 c, int sw, int 
   return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w, t, c, 0, 0, 0, sw, 0, st);   // both e4m3, byte 0 of the scales
 }
 
-// dma16_to_lds with 4 bytes per lane
-__device__ __forceinline__ void dma4_to_lds(const void *base, unsigned voff, unsigned lds_addr) {
+// A wavefront-wide copy of 4 bytes per lane straight into LDS: lane i's at LDS byte address lds_addr + 4 i (lds_addr uniform).  Lanes that are
+// switched off copy nothing.  Completion as for dma16_to_lds.
+__device__ __forceinline__ void dma4_to_lds(const void *from, unsigned lds_addr) {
   lds_addr = __builtin_amdgcn_readfirstlane(lds_addr);
-  asm volatile("s_nop 0\n\tglobal_load_lds_dword %0, %1"
+  asm volatile("s_nop 0\n\tglobal_load_lds_dword %0, off"
                :
-               : "v"(voff), "s"(base), "{m0}"(lds_addr)
+               : "v"(from), "{m0}"(lds_addr)
                : "memory");
 }
 
@@ -99,24 +100,19 @@ __global__ __launch_bounds__(64 * WM * WN * KG, KG > 1 ? WM * WN * KG / 4 : 2) v
   auto feature_of = [](int w) { return (w & ~31) + 8 * ((w & 15) >> 2) + 4 * ((w >> 4) & 1) + (w & 3); };
   auto source = [&](int row) { return row < BM ? min(row, M - 1 - m0) : min(feature_of(row - BM), N - 1 - n0); };   // in the tile
   const unsigned char *A = p.A + m0 * p.lda, *W = p.W + n0 * p.ldw;
-  const unsigned char *sa = p.sa + m0 * p.lsa, *sw8 = p.sw + n0 * p.lsw;
   unsigned voff[MYR];
   const int cq = (lane & 7) ^ gemm_swizzle(8 * wave + (lane >> 3));   // 8 NW rows further the swizzle is the same
   static_assert(NW % 2 == 0, "swizzle period of 16 rows");
 #pragma unroll
   for (int i = 0; i < MYR; ++i)
     voff[i] = (unsigned)(source(8 * (wave + NW * i) + (lane >> 3)) * (i < TOKR ? p.lda : p.ldw) + 16 * cq);
-  // scales: wavefront w copies those of stage rows SPW w .. SPW w + SPW - 1; a run that reaches over both operands takes two copies
+  // scales: wavefront w copies those of stage rows SPW w .. SPW w + SPW - 1
   const int srow = SPW * wave + (lane < SPW ? lane : 0);
-  const bool s_tok = srow < BM;
-  const unsigned soff = (unsigned)(source(srow) * (s_tok ? p.lsa : p.lsw));
-  constexpr bool MIXED = BM % SPW != 0;
-  static_assert(!MIXED, "a wavefront's scales belong to one operand");
-  const bool tok_wave = SPW * wave < BM;
+  const unsigned char *scales = srow < BM ? p.sa + (m0 + source(srow)) * p.lsa : p.sw + (n0 + source(srow)) * p.lsw;
   auto issue = [&](int kt, int stage) __attribute__((always_inline)) {
     const int k = __builtin_amdgcn_readfirstlane(kt);
     const unsigned to = lds0 + STAGE * stage;
-    if (lane < SPW) dma4_to_lds((tok_wave ? sa : sw8) + (k & ~3), soff, to + 128 * ROWS + 4 * SPW * wave);
+    if (lane < SPW) dma4_to_lds(scales + (k & ~3), to + 128 * ROWS + 4 * SPW * wave);
 #pragma unroll
     for (int i = 0; i < MYR; ++i) dma16_to_lds((i < TOKR ? A : W) + 128LL * k, voff[i], to + 1024 * (wave + NW * i));
   };

@@ -23,10 +23,13 @@
 #include "gemm_tile.hpp"
 #include "launch_plan.hpp"
 #include "module_rowwise.hpp"
+#include "pab_internal.hpp"
 
 namespace {
-
 thread_local char g_err[512] = "";
+}
+
+namespace pab {
 
 int fail(int code, const char *fmt, ...) {
   va_list ap;
@@ -36,8 +39,14 @@ int fail(int code, const char *fmt, ...) {
   return code;
 }
 
+}  // namespace pab
+
+namespace {
+
+using pab::aligned16;
+using pab::fail;
+
 bool kind_ok(int kind) { return kind == PAB_SPATIAL || kind == PAB_TEMPORAL || kind == PAB_CROSS; }
-bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 size_t elem_size(int dtype) { return dtype == PAB_BF16 ? 2 : 4; }
 
 // ---- launches -----------------------------------------------------------------
@@ -291,14 +300,56 @@ struct pab_ctx {
   std::vector<int> last_step;      // per (block, kind): last step seen since reset, -1 if none
   std::vector<int> computed_step;  // per (block, kind): step whose output the slot holds, -1 if none
   long long launches;
+  bool quantized;        // slots hold 8-bit rows
 };
 
 namespace {
 
-// ---- what the two cached entry points share: validate the cell, take the decision of Eq. 1,
+size_t slots_of(const pab_config &c) {
+  size_t slots = 0;
+  for (int b = 0; b < c.n_blocks; ++b) slots += (size_t)__builtin_popcount(kinds_of_block(c, b));
+  return slots;
+}
+
+// a slot of 8-bit rows [T * S, heads * head_dim]
+size_t quantized_slot_bytes_of(const pab_config &c) { return pab::q8_bytes((long long)c.T * c.S, (long long)c.heads * c.head_dim); }
+
+int create_context(const pab_config *cfg, void *workspace, size_t workspace_bytes, bool quantized, pab_ctx **out) {
+  if (!out) return fail(PAB_EINVAL, "out is NULL");
+  *out = nullptr;
+  const int rc = check_config(cfg);
+  if (rc != PAB_OK) return rc;
+  if (!workspace) return fail(PAB_EINVAL, "workspace is NULL");
+  if (reinterpret_cast<uintptr_t>(workspace) & 255u) return fail(PAB_EINVAL, "workspace must be 256-byte aligned");
+  const size_t slot = quantized ? quantized_slot_bytes_of(*cfg) : slot_bytes_of(*cfg), need = slot * slots_of(*cfg);
+  if (!slot) return fail(PAB_EINVAL, "slots too large");
+  if (workspace_bytes < need)
+    return fail(PAB_ENOMEM, "workspace has %zu bytes, the cache needs %zu", workspace_bytes, need);
+  pab_ctx *ctx = new (std::nothrow) pab_ctx;
+  if (!ctx) return fail(PAB_ENOMEM, "out of host memory");
+  ctx->cfg = *cfg;
+  ctx->workspace = static_cast<unsigned char *>(workspace);
+  ctx->slot_bytes = slot;
+  ctx->quantized = quantized;
+  ctx->slot_index.assign((size_t)cfg->n_blocks * 3, -1);
+  long long next = 0;
+  for (int b = 0; b < cfg->n_blocks; ++b)
+    for (int k = 0; k < 3; ++k)
+      if ((kinds_of_block(*cfg, b) >> k) & 1) ctx->slot_index[(size_t)b * 3 + k] = next++;
+  ctx->cfg.block_kinds = nullptr;   // the caller's array is not kept
+  ctx->last_step.assign((size_t)cfg->n_blocks * 3, -1);
+  ctx->computed_step.assign((size_t)cfg->n_blocks * 3, -1);
+  ctx->launches = 0;
+  *out = ctx;
+  return PAB_OK;
+}
+
+// ---- what the cached entry points share: validate the cell, take the decision of Eq. 1,
 //      find the slot; after a successful launch (or on reuse) record the step ----
-int schedule_cell(pab_ctx *ctx, int block, int kind, int step, void **slot) {
+int schedule_cell(pab_ctx *ctx, int block, int kind, int step, bool quantized, void **slot) {
   const pab_config &c = ctx->cfg;
+  if (ctx->quantized != quantized)
+    return fail(PAB_EINVAL, ctx->quantized ? "the context's slots hold 8-bit rows: use the calls for those" : "the context's slots do not hold 8-bit rows");
   if (!kind_ok(kind)) return fail(PAB_EINVAL, "kind %d is not spatial(0)/temporal(1)/cross(2)", kind);
   if (c.interval[kind] == 0) return fail(PAB_EINVAL, "kind %d is absent from this config (interval 0)", kind);
   if (block < 0 || block >= c.n_blocks) return fail(PAB_EINVAL, "block %d outside [0, %d)", block, c.n_blocks);
@@ -806,37 +857,20 @@ int pab_preset(int model, int level, int interval[3], double *t_start, double *t
 
 size_t pab_workspace_bytes(const pab_config *cfg) {
   if (check_config(cfg) != PAB_OK) return 0;
-  size_t slots = 0;
-  for (int b = 0; b < cfg->n_blocks; ++b) slots += (size_t)__builtin_popcount(kinds_of_block(*cfg, b));
-  return slot_bytes_of(*cfg) * slots;
+  return slot_bytes_of(*cfg) * slots_of(*cfg);
+}
+
+size_t pab_workspace_bytes_quantized(const pab_config *cfg) {
+  if (check_config(cfg) != PAB_OK) return 0;
+  return quantized_slot_bytes_of(*cfg) * slots_of(*cfg);
 }
 
 int pab_create(const pab_config *cfg, void *workspace, size_t workspace_bytes, pab_ctx **out) {
-  if (!out) return fail(PAB_EINVAL, "out is NULL");
-  *out = nullptr;
-  const int rc = check_config(cfg);
-  if (rc != PAB_OK) return rc;
-  if (!workspace) return fail(PAB_EINVAL, "workspace is NULL");
-  if (reinterpret_cast<uintptr_t>(workspace) & 255u) return fail(PAB_EINVAL, "workspace must be 256-byte aligned");
-  const size_t need = pab_workspace_bytes(cfg);
-  if (workspace_bytes < need)
-    return fail(PAB_ENOMEM, "workspace has %zu bytes, the cache needs %zu", workspace_bytes, need);
-  pab_ctx *ctx = new (std::nothrow) pab_ctx;
-  if (!ctx) return fail(PAB_ENOMEM, "out of host memory");
-  ctx->cfg = *cfg;
-  ctx->workspace = static_cast<unsigned char *>(workspace);
-  ctx->slot_bytes = slot_bytes_of(*cfg);
-  ctx->slot_index.assign((size_t)cfg->n_blocks * 3, -1);
-  long long next = 0;
-  for (int b = 0; b < cfg->n_blocks; ++b)
-    for (int k = 0; k < 3; ++k)
-      if ((kinds_of_block(*cfg, b) >> k) & 1) ctx->slot_index[(size_t)b * 3 + k] = next++;
-  ctx->cfg.block_kinds = nullptr;   // the caller's array is not kept
-  ctx->last_step.assign((size_t)cfg->n_blocks * 3, -1);
-  ctx->computed_step.assign((size_t)cfg->n_blocks * 3, -1);
-  ctx->launches = 0;
-  *out = ctx;
-  return PAB_OK;
+  return create_context(cfg, workspace, workspace_bytes, false, out);
+}
+
+int pab_create_quantized(const pab_config *cfg, void *workspace, size_t workspace_bytes, pab_ctx **out) {
+  return create_context(cfg, workspace, workspace_bytes, true, out);
 }
 
 int pab_reset(pab_ctx *ctx) {
@@ -860,7 +894,7 @@ int pab_attention(pab_ctx *ctx, int block, int kind, int step, const void *q, co
   *out = nullptr;
   const pab_config &c = ctx->cfg;
   void *slot = nullptr;
-  const int decision = schedule_cell(ctx, block, kind, step, &slot);
+  const int decision = schedule_cell(ctx, block, kind, step, false, &slot);
   if (decision < 0) return decision;
   if (decision == PAB_COMPUTE) {
     if (!q || !k || !v) return fail(PAB_EINVAL, "q, k, v must be non-NULL on a computed step");
@@ -932,7 +966,7 @@ int pab_module_attention(pab_ctx *ctx, int block, int kind, int step, const void
   const pab_config &c = ctx->cfg;
   if (c.dtype != PAB_BF16) return fail(PAB_EINVAL, "the module path takes bf16 configs only");
   void *slot = nullptr;
-  const int decision = schedule_cell(ctx, block, kind, step, &slot);
+  const int decision = schedule_cell(ctx, block, kind, step, false, &slot);
   if (decision < 0) return decision;
   if (decision == PAB_COMPUTE) {
     const int rc = launch_module(kind, c.T, c.S, c.L, c.heads, c.head_dim, x, text, w, scratch, scratch_bytes, slot,
@@ -941,6 +975,76 @@ int pab_module_attention(pab_ctx *ctx, int block, int kind, int step, const void
   }
   commit_cell(ctx, block, kind, step, decision);
   *out = slot;
+  return decision;
+}
+
+int pab_slot_quantized(const pab_ctx *ctx, int block, int kind, pab_q8 *out) {
+  if (!ctx || !out) return fail(PAB_EINVAL, "ctx and out must not be NULL");
+  if (!ctx->quantized) return fail(PAB_EINVAL, "the context's slots do not hold 8-bit rows");
+  void *slot = const_cast<void *>(pab_slot_ptr(ctx, block, kind));
+  if (!slot) return fail(PAB_EINVAL, "block %d has no attention of kind %d", block, kind);
+  const pab_config &c = ctx->cfg;
+  *out = pab::q8_at(slot, (long long)c.T * c.S, (long long)c.heads * c.head_dim);
+  return PAB_OK;
+}
+
+int pab_attention_quantized(pab_ctx *ctx, int block, int kind, int step, const void *q, const void *k, const void *v, void *scratch,
+                            size_t scratch_bytes, void *hip_stream, pab_q8 *out) {
+  if (!ctx) return fail(PAB_EINVAL, "ctx is NULL");
+  if (!out) return fail(PAB_EINVAL, "out is NULL");
+  *out = pab_q8{};
+  const pab_config &c = ctx->cfg;
+  void *slot = nullptr;
+  const int decision = schedule_cell(ctx, block, kind, step, true, &slot);
+  if (decision < 0) return decision;
+  const long long tok = (long long)c.T * c.S;
+  const int C = c.heads * c.head_dim;
+  const pab_q8 rows = pab::q8_at(slot, tok, C);
+  if (decision == PAB_COMPUTE) {
+    if (!q || !k || !v || !scratch) return fail(PAB_EINVAL, "q, k, v and scratch must be non-NULL on a computed step");
+    if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(scratch))
+      return fail(PAB_EINVAL, "q, k, v and scratch must be 16-byte aligned");
+    const size_t need = (size_t)tok * C * elem_size(c.dtype);
+    if (scratch_bytes < need) return fail(PAB_ENOMEM, "scratch of %zu bytes, need %zu", scratch_bytes, need);
+    const hipStream_t st = static_cast<hipStream_t>(hip_stream);
+    int rc = launch_checked(kind, c.dtype, c.T, c.S, c.L, c.heads, c.head_dim, q, k, v, scratch, st);
+    if (rc == PAB_OK) rc = pab::quantize(tok, C, c.dtype, scratch, C, &rows, st);
+    if (rc != PAB_OK) {
+      ctx->computed_step[(size_t)block * 3 + kind] = -1;   // the slot may hold parts of it
+      return rc;
+    }
+  }
+  commit_cell(ctx, block, kind, step, decision);
+  *out = rows;
+  return decision;
+}
+
+int pab_module_attention_quantized(pab_ctx *ctx, int block, int kind, int step, const void *x, const void *text,
+                                   const pab_module_weights *w, void *scratch, size_t scratch_bytes, void *hip_stream, pab_q8 *out) {
+  if (!ctx) return fail(PAB_EINVAL, "ctx is NULL");
+  if (!out) return fail(PAB_EINVAL, "out is NULL");
+  *out = pab_q8{};
+  const pab_config &c = ctx->cfg;
+  if (c.dtype != PAB_BF16) return fail(PAB_EINVAL, "the module path takes bf16 configs only");
+  void *slot = nullptr;
+  const int decision = schedule_cell(ctx, block, kind, step, true, &slot);
+  if (decision < 0) return decision;
+  const long long tok = (long long)c.T * c.S;
+  const int C = c.heads * c.head_dim;
+  const pab_q8 rows = pab::q8_at(slot, tok, C);
+  if (decision == PAB_COMPUTE) {
+    // the query plane is free once the attention has run: the output projection leaves its result there
+    const hipStream_t st = static_cast<hipStream_t>(hip_stream);
+    unsigned char *y = static_cast<unsigned char *>(scratch) + module_plane_bytes(c.T, c.S, c.L, c.heads, c.head_dim);
+    int rc = launch_module(kind, c.T, c.S, c.L, c.heads, c.head_dim, x, text, w, scratch, scratch_bytes, y, st);
+    if (rc == PAB_OK) rc = pab::quantize(tok, C, PAB_BF16, y, C, &rows, st);
+    if (rc != PAB_OK) {
+      ctx->computed_step[(size_t)block * 3 + kind] = -1;
+      return rc;
+    }
+  }
+  commit_cell(ctx, block, kind, step, decision);
+  *out = rows;
   return decision;
 }
 

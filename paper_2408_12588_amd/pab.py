@@ -24,6 +24,8 @@ SPATIAL, TEMPORAL, CROSS = 0, 1, 2
 COMPUTE, REUSE = 0, 1
 OK, EINVAL, ESTATE, ENOMEM, EDEVICE = 0, -1, -2, -3, -4
 BF16, F32 = 0, 1
+NONE, GELU = 0, 1                              # activations
+NORM_NONE, NORM_LAYER, NORM_RMS = 0, 1, 2
 
 EXPORTS = (
     "pab_schedule", "pab_source_step", "pab_window_from_timesteps", "pab_preset", "pab_workspace_bytes", "pab_create", "pab_reset", "pab_attention",
@@ -32,6 +34,10 @@ EXPORTS = (
     "pab_mlp_schedule", "pab_mlp_source_step", "pab_steps_from_timesteps", "pab_mlp_scratch_bytes", "pab_mlp_compute",
     "pab_mlp_workspace_bytes", "pab_mlp_create", "pab_mlp_reset", "pab_mlp", "pab_mlp_launch_count", "pab_mlp_slot_ptr",
     "pab_mlp_destroy",
+    "pab_quantized_bytes", "pab_quantized_layout", "pab_quantize", "pab_dequantize", "pab_linear_quantized",
+    "pab_mlp_scratch_bytes_quantized", "pab_mlp_compute_quantized",
+    "pab_workspace_bytes_quantized", "pab_create_quantized", "pab_attention_quantized", "pab_module_attention_quantized",
+    "pab_slot_quantized", "pab_qk_norm_rope", "pab_rope_factors_count", "pab_rope_factors",
     "pab_launch_count", "pab_slot_ptr", "pab_destroy", "pab_last_error",
 )
 
@@ -63,6 +69,23 @@ class pab_mlp_config(ctypes.Structure):
     _fields_ = [("n_blocks", ctypes.c_int), ("n_steps", ctypes.c_int), ("n_tok", ctypes.c_longlong),
                 ("hidden", ctypes.c_int), ("inner", ctypes.c_int), ("n_starts", ctypes.c_int), ("range", ctypes.c_int),
                 ("block_lo", ctypes.c_int), ("block_hi", ctypes.c_int)]
+
+
+class pab_q8(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("scale", ctypes.c_void_p), ("ld", ctypes.c_longlong), ("ld_scale", ctypes.c_longlong)]
+
+
+class pab_mlp_weights_quantized(ctypes.Structure):
+    _fields_ = [("shift", ctypes.c_void_p), ("scale", ctypes.c_void_p), ("w1", pab_q8), ("b1", ctypes.c_void_p), ("w2", pab_q8),
+                ("b2", ctypes.c_void_p)]
+
+
+class pab_qk_norm(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_int) for n in ("dtype", "norm", "n_batch", "heads_q", "heads_k", "head_dim")]
+                + [("places", ctypes.c_int * 3), ("axis_dim", ctypes.c_int * 3), ("eps", ctypes.c_float)]
+                + [(n, ctypes.c_void_p) for n in ("q", "k", "q_out", "k_out")]
+                + [(n, ctypes.c_longlong) for n in ("ld_q", "ld_k", "ld_q_out", "ld_k_out")]
+                + [(n, ctypes.c_void_p) for n in ("gamma_q", "beta_q", "gamma_k", "beta_k", "factors")])
 
 
 def _load() -> ctypes.CDLL:
@@ -129,6 +152,25 @@ def _load() -> ctypes.CDLL:
     lib.pab_mlp_slot_ptr.argtypes = [vp, ci]
     lib.pab_mlp_destroy.restype = ci
     lib.pab_mlp_destroy.argtypes = [vp]
+    q8p, ll, sz, cfgp = ctypes.POINTER(pab_q8), ctypes.c_longlong, ctypes.c_size_t, ctypes.POINTER(pab_config)
+    for name, restype, argtypes in (
+            ("pab_quantized_bytes", sz, [ll, ci]),
+            ("pab_quantized_layout", ci, [ll, ci, vp, sz, q8p]),
+            ("pab_quantize", ci, [ll, ci, ci, vp, ll, q8p, vp]),
+            ("pab_dequantize", ci, [ll, ci, ci, q8p, vp, ll, vp, vp, ll, vp]),
+            ("pab_linear_quantized", ci, [ci, ci, ci, q8p, q8p, vp, ci, vp, ll, q8p, vp]),
+            ("pab_mlp_scratch_bytes_quantized", sz, [ll, ci, ci]),
+            ("pab_mlp_compute_quantized", ci, [ll, ci, ci, vp, ctypes.POINTER(pab_mlp_weights_quantized), vp, sz, vp, vp]),
+            ("pab_workspace_bytes_quantized", sz, [cfgp]),
+            ("pab_create_quantized", ci, [cfgp, vp, sz, ctypes.POINTER(vp)]),
+            ("pab_attention_quantized", ci, [vp, ci, ci, ci, vp, vp, vp, vp, sz, vp, q8p]),
+            ("pab_module_attention_quantized", ci, [vp, ci, ci, ci, vp, vp, ctypes.POINTER(pab_module_weights), vp, sz, vp, q8p]),
+            ("pab_slot_quantized", ci, [vp, ci, ci, q8p]),
+            ("pab_qk_norm_rope", ci, [ctypes.POINTER(pab_qk_norm), vp]),
+            ("pab_rope_factors_count", ll, [ip, ip]),
+            ("pab_rope_factors", ci, [ip, ip, dp, dp, ctypes.c_double, vp, vp])):
+        getattr(lib, name).restype = restype
+        getattr(lib, name).argtypes = argtypes
     lib.pab_launch_count.restype = ctypes.c_longlong
     lib.pab_launch_count.argtypes = [vp]
     lib.pab_slot_ptr.restype = vp
@@ -538,3 +580,304 @@ class MlpContext:
             self.pab_mlp_destroy()
         except Exception:
             pass
+
+
+# ---- 8-bit rows -------------------------------------------------------------------------------
+def _rows_of(t, name):
+    """(rows, columns, row pitch in elements) of a device tensor whose last axis is dense and whose leading axes collapse."""
+    if not t.is_cuda:
+        raise ValueError("libpab takes device tensors (%s)" % name)
+    if t.dim() == 0 or t.stride(-1) != 1 and t.shape[-1] != 1:
+        raise ValueError("%s needs a dense last axis" % name)
+    K = t.shape[-1]
+    if t.is_contiguous():
+        return (t.numel() // K if K else 0), K, K
+    lead = [(n, st) for n, st in zip(t.shape[:-1], t.stride()[:-1]) if n != 1]
+    if any(a[1] != b[1] * b[0] for a, b in zip(lead, lead[1:])):
+        raise ValueError("the leading axes of %s must collapse into one row index" % name)
+    rows = 1
+    for n, _ in lead:
+        rows *= n
+    return rows, K, (lead[-1][1] if lead else K)
+
+
+def _float_type(t, name):
+    if t.dtype is torch.bfloat16:
+        return BF16
+    if t.dtype is torch.float32:
+        return F32
+    raise ValueError("%s must be bf16 or f32" % name)
+
+
+def _same_device(first, *others):
+    """All on the current device: launches go to its current stream."""
+    i = first.get_device()
+    if any(t is not None and t.get_device() != i for t in others):
+        raise ValueError("the tensors are on different devices")
+    if i != torch.cuda.current_device():
+        raise ValueError("the tensors are on device %d, the current device is %d" % (i, torch.cuda.current_device()))
+
+
+def _new(shape, dtype, device, stream):
+    """A tensor that belongs to the stream on which the launch will write it."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    if isinstance(stream, int):
+        stream = torch.cuda.ExternalStream(stream, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
+class Q8:
+    """8-bit rows: ``data`` [rows, >= K rounded up to 128] (uint8 or e4m3), ``scale`` [rows, ...] exponent bytes (uint8), device
+    tensors that this object keeps; ``K`` columns of values."""
+    __slots__ = ("data", "scale", "K", "struct")
+
+    def __init__(self, data, scale, K: int):
+        if data.dim() != 2 or scale.dim() != 2 or data.element_size() != 1 or scale.element_size() != 1:
+            raise ValueError("data and scale are matrices of bytes")
+        if not data.is_cuda or not scale.is_cuda:
+            raise ValueError("libpab takes device tensors")
+        if data.get_device() != scale.get_device():
+            raise ValueError("data and scale are on different devices")
+        if data.shape[0] != scale.shape[0]:
+            raise ValueError("data has %d rows, scale %d" % (data.shape[0], scale.shape[0]))
+        nb = (K + 127) // 128
+        if K < 1 or data.shape[1] < 128 * nb or scale.shape[1] < nb or data.stride(1) != 1 or scale.stride(1) != 1:
+            raise ValueError("K=%d wants dense rows of at least %d bytes and %d scales" % (K, 128 * nb, nb))
+        self.data, self.scale, self.K = data, scale, K
+        self.struct = pab_q8(data.data_ptr(), scale.data_ptr(), data.stride(0), scale.stride(0))
+
+    @property
+    def rows(self) -> int:
+        return self.data.shape[0]
+
+
+def q8_empty(rows: int, K: int, device="cuda:0", stream=None) -> Q8:
+    """Uninitialised 8-bit rows."""
+    nb = (K + 127) // 128
+    return Q8(_new((rows, 128 * nb), torch.uint8, device, stream), _new((rows, (nb + 3) // 4 * 4), torch.uint8, device, stream), K)
+
+
+def pab_quantized_bytes(rows: int, K: int) -> int:
+    return lib.pab_quantized_bytes(rows, K)
+
+
+def q8_view(buffer, rows: int, K: int) -> Q8:
+    """8-bit rows in one uint8 tensor of pab_quantized_bytes, as pab_quantized_layout places them."""
+    s = pab_q8()
+    _check(lib.pab_quantized_layout(rows, K, _ptr(buffer), buffer.numel(), ctypes.byref(s)))
+    return _q8_inside(buffer, s, rows, K)
+
+
+def _q8_inside(buffer, s: pab_q8, rows: int, K: int) -> Q8:
+    a, b = s.data - buffer.data_ptr(), s.scale - buffer.data_ptr()
+    return Q8(buffer[a:a + rows * s.ld].view(rows, s.ld), buffer[b:b + rows * s.ld_scale].view(rows, s.ld_scale), K)
+
+
+def pab_quantize(x, out: Q8 | None = None, stream=None) -> Q8:
+    """x ``[..., K]`` bf16 or f32 (dense last axis) -> 8-bit rows."""
+    dtype = _float_type(x, "x")
+    rows, K, ldx = _rows_of(x, "x")
+    if out is None:
+        out = q8_empty(rows, K, x.device, stream)
+    elif out.rows != rows or out.K != K:
+        raise ValueError("out holds [%d, %d], x is [%d, %d]" % (out.rows, out.K, rows, K))
+    _same_device(x, out.data)
+    _check(lib.pab_quantize(rows, K, dtype, x.data_ptr(), ldx, out.struct, _stream(stream)))
+    return out
+
+
+def pab_dequantize(y: Q8, x=None, gate=None, dtype=None, out=None, stream=None):
+    """out = x + gate * y: x ``[..., K]`` or None (0), gate ``[K]`` or None (1); type and shape of x, else ``dtype`` (bf16) and [rows, K]."""
+    if dtype is None:
+        dtype = x.dtype if x is not None else out.dtype if out is not None else torch.bfloat16
+    ldx = 0
+    if x is not None:
+        rows, K, ldx = _rows_of(x, "x")
+        if (rows, K) != (y.rows, y.K) or x.dtype != dtype:
+            raise ValueError("x must be [%d, %d] of %s" % (y.rows, y.K, dtype))
+    if gate is not None and (gate.dtype != dtype or gate.numel() != y.K or not gate.is_contiguous()):
+        raise ValueError("gate must be a dense [%d] of %s" % (y.K, dtype))
+    if out is None:
+        out = _new(x.shape if x is not None else (y.rows, y.K), dtype, y.data.device, stream)
+    rows, K, ldo = _rows_of(out, "out")
+    if (rows, K) != (y.rows, y.K) or out.dtype != dtype:
+        raise ValueError("out must be [%d, %d] of %s" % (y.rows, y.K, dtype))
+    _same_device(y.data, x, gate, out)
+    _check(lib.pab_dequantize(rows, K, _float_type(out, "out"), y.struct, 0 if x is None else x.data_ptr(), ldx,
+                              0 if gate is None else gate.data_ptr(), out.data_ptr(), ldo, _stream(stream)))
+    return out
+
+
+def pab_linear_quantized(a: Q8, w: Q8, bias=None, act: int = NONE, out=None, stream=None):
+    """act(a @ w.T + bias) of 8-bit rows a [M, K], w [N, K]; bias ``[N]`` bf16 or None.  ``out``: a bf16 tensor ``[..., N]`` (new if None),
+    or a ``Q8`` [M, N] that the result is quantised into."""
+    M, N, K = a.rows, w.rows, a.K
+    if w.K != K:
+        raise ValueError("a has %d columns, w %d" % (K, w.K))
+    if bias is not None and (bias.dtype is not torch.bfloat16 or bias.numel() != N or not bias.is_contiguous()):
+        raise ValueError("bias must be a dense [%d] of bf16" % N)
+    if out is None:
+        out = _new((M, N), torch.bfloat16, a.data.device, stream)
+    if isinstance(out, Q8):
+        if out.rows != M or out.K != N:
+            raise ValueError("out holds [%d, %d], the product is [%d, %d]" % (out.rows, out.K, M, N))
+        c, ldc, c8, where = 0, 0, out.struct, out.data
+    else:
+        rows, cols, ldc = _rows_of(out, "out")
+        if (rows, cols) != (M, N) or out.dtype is not torch.bfloat16:
+            raise ValueError("out must be [%d, %d] of bf16" % (M, N))
+        c, c8, where = out.data_ptr(), None, out
+    _same_device(a.data, w.data, bias, where)
+    _check(lib.pab_linear_quantized(M, N, K, a.struct, w.struct, 0 if bias is None else bias.data_ptr(), act, c, ldc, c8, _stream(stream)))
+    return out
+
+
+def mlp_weights_quantized(shift, scale, w1: Q8, b1, w2: Q8, b2) -> pab_mlp_weights_quantized:
+    """Weights of pab_mlp_compute_quantized: shift, scale ``[hidden]``, b1 ``[inner]``, b2 ``[hidden]`` bf16 (b1, b2 may be None), w1, w2 8-bit
+    rows; kept alive on the result."""
+    hidden, inner = w1.K, w1.rows
+    if w2.rows != hidden or w2.K != inner:
+        raise ValueError("w1 is [%d, %d], w2 [%d, %d]" % (inner, hidden, w2.rows, w2.K))
+    for name, t, n in (("shift", shift, hidden), ("scale", scale, hidden), ("b1", b1, inner), ("b2", b2, hidden)):
+        if t is None and name in ("b1", "b2"):
+            continue
+        if t.dtype is not torch.bfloat16 or t.numel() != n:
+            raise ValueError("%s must be [%d] of bf16" % (name, n))
+    w = pab_mlp_weights_quantized(_ptr(shift), _ptr(scale), w1.struct, _ptr(b1), w2.struct, _ptr(b2))
+    w._keep = (shift, scale, w1, b1, w2, b2)
+    w._shape = (hidden, inner)
+    return w
+
+
+def pab_mlp_scratch_bytes_quantized(n_tok: int, hidden: int, inner: int) -> int:
+    return lib.pab_mlp_scratch_bytes_quantized(n_tok, hidden, inner)
+
+
+def pab_mlp_compute_quantized(x, w: pab_mlp_weights_quantized, scratch=None, out=None, stream=None):
+    """One MLP module on 8-bit rows, without schedule or cache: x ``[..., hidden]`` bf16 -> same shape."""
+    hidden, inner = w._shape
+    if x.dtype is not torch.bfloat16 or x.shape[-1] != hidden:
+        raise ValueError("x must be [..., %d] of bf16" % hidden)
+    n_tok = x.numel() // hidden
+    if scratch is None:
+        scratch = _new((lib.pab_mlp_scratch_bytes_quantized(n_tok, hidden, inner),), torch.uint8, x.device, stream)
+    if out is None:
+        out = _new(x.shape, torch.bfloat16, x.device, stream)
+    if out.dtype is not torch.bfloat16 or out.shape != x.shape:
+        raise ValueError("out must have the shape and type of x")
+    _same_device(x, w._keep[2].data, scratch, out)
+    _check(lib.pab_mlp_compute_quantized(n_tok, hidden, inner, _ptr(x), ctypes.byref(w), _ptr(scratch), scratch.numel(), _ptr(out),
+                                         _stream(stream)))
+    return out
+
+
+class QuantizedContext(PabContext):
+    """A broadcast cache of 8-bit rows: pab_create_quantized and the calls that go with it."""
+
+    def __init__(self, cfg: pab_config, device="cuda:0", workspace: torch.Tensor | None = None):
+        self.cfg, self._h, self._address = cfg, None, None
+        need = lib.pab_workspace_bytes_quantized(ctypes.byref(cfg))
+        if need == 0:
+            raise PabError(EINVAL, pab_last_error())
+        if workspace is None:
+            workspace = torch.empty(need, dtype=torch.uint8, device=device)
+        self.workspace = workspace
+        handle = ctypes.c_void_p()
+        _check(lib.pab_create_quantized(ctypes.byref(cfg), workspace.data_ptr(), workspace.numel(), ctypes.byref(handle)))
+        self._h = handle
+        self._address = handle.value
+        self.shape = (cfg.T, cfg.S, cfg.heads, cfg.head_dim)
+        self.dtype = _TORCH_DTYPE[cfg.dtype]
+        self._numel = cfg.T * cfg.S * cfg.heads * cfg.head_dim
+
+    def slot_tensor(self, block: int, kind: int) -> Q8:
+        """Cache slot (block, kind) inside the workspace tensor (no copy)."""
+        s = pab_q8()
+        _check(lib.pab_slot_quantized(self._h, block, kind, ctypes.byref(s)))
+        return _q8_inside(self.workspace, s, self.cfg.T * self.cfg.S, self.cfg.heads * self.cfg.head_dim)
+
+    def pab_attention_quantized(self, block: int, kind: int, step: int, q, k, v, scratch, stream=None):
+        """-> (decision, the slot as 8-bit rows).  scratch: uint8, the bytes of one output tensor (computed steps)."""
+        s = pab_q8()
+        dec = _check(lib.pab_attention_quantized(self._h, block, kind, step, _ptr(q), _ptr(k), _ptr(v), _ptr(scratch),
+                                                 scratch.numel() if scratch is not None else 0, _stream(stream), ctypes.byref(s)))
+        return dec, _q8_inside(self.workspace, s, self.cfg.T * self.cfg.S, self.cfg.heads * self.cfg.head_dim)
+
+    def pab_module_attention_quantized(self, block: int, kind: int, step: int, x, text, w, scratch, stream=None):
+        """Module-level call -> (decision, the slot as 8-bit rows); scratch as for pab_module_attention."""
+        s = pab_q8()
+        dec = _check(lib.pab_module_attention_quantized(
+            self._h, block, kind, step, _ptr(x), _ptr(text), ctypes.byref(w) if w is not None else None, _ptr(scratch),
+            scratch.numel() if scratch is not None else 0, _stream(stream), ctypes.byref(s)))
+        return dec, _q8_inside(self.workspace, s, self.cfg.T * self.cfg.S, self.cfg.heads * self.cfg.head_dim)
+
+
+# ---- query / key norm with rotation over several axes -----------------------------------------
+def pab_rope_factors_count(places, axis_dim) -> int:
+    return _check(lib.pab_rope_factors_count(_int_array(places), _int_array(axis_dim)))
+
+
+def pab_rope_factors(places, axis_dim, origin=(0.0, 0.0, 0.0), step=(1.0, 1.0, 1.0), theta: float = 10000.0, device="cuda:0", stream=None):
+    """The table of pab_qk_norm_rope, fp32 ``[count, 2]``: built once for a video's shape."""
+    if not len(places) == len(axis_dim) == len(origin) == len(step) == 3:
+        raise ValueError("three axes (one place and no features for an axis that a model lacks)")
+    n = pab_rope_factors_count(places, axis_dim)
+    out = _new((n, 2), torch.float32, device, stream)
+    three = ctypes.c_double * 3
+    if n:
+        _same_device(out)
+    _check(lib.pab_rope_factors(_int_array(places), _int_array(axis_dim), three(*origin), three(*step), theta, out.data_ptr(), _stream(stream)))
+    return out
+
+
+def _heads_of(t, name):
+    """(tokens, heads, head dim, token pitch) of ``[..., H, D]`` whose heads are dense."""
+    if t.dim() < 3 or not t.is_cuda:
+        raise ValueError("%s must be a device tensor [..., heads, head_dim]" % name)
+    H, D = t.shape[-2:]
+    if t.is_contiguous():
+        return t.numel() // max(H * D, 1), H, D, H * D
+    if t.stride(-1) != 1 or (H > 1 and t.stride(-2) != D):
+        raise ValueError("the heads of %s must be dense" % name)
+    lead = [(n, st) for n, st in zip(t.shape[:-2], t.stride()[:-2]) if n != 1]
+    if any(a[1] != b[1] * b[0] for a, b in zip(lead, lead[1:])):
+        raise ValueError("the leading axes of %s must collapse into one token index" % name)
+    n = 1
+    for m, _ in lead:
+        n *= m
+    return n, H, D, (lead[-1][1] if lead else H * D)
+
+
+def pab_qk_norm_rope(q, k, places, axis_dim, factors=None, norm: int = NORM_LAYER, gamma_q=None, beta_q=None, gamma_k=None, beta_k=None,
+                     eps: float = 1e-6, q_out=None, k_out=None, stream=None):
+    """Norm per head and rotation of q ``[..., Hq, D]`` and k ``[..., Hk, D]`` (or None), tokens in the order of the grid ``places`` (times a
+    batch); ``factors`` from pab_rope_factors (None: no rotation).  -> (q_out, k_out); they may be q and k."""
+    n, Hq, D, ld_q = _heads_of(q, "q")
+    dtype = _float_type(q, "q")
+    grid = places[0] * places[1] * places[2]
+    if grid < 1 or n % grid or n == 0:
+        raise ValueError("%d tokens are no batch of grids of %s" % (n, tuple(places)))
+    if factors is not None and (factors.dtype is not torch.float32 or not factors.is_contiguous()
+                                or factors.numel() != 2 * sum(p * (a // 2) for p, a in zip(places, axis_dim))):
+        raise ValueError("factors must be the dense f32 table of these places and sections")
+    for name, t in (("gamma_q", gamma_q), ("beta_q", beta_q), ("gamma_k", gamma_k), ("beta_k", beta_k)):
+        if t is not None and (t.dtype != q.dtype or t.numel() != D or not t.is_contiguous()):
+            raise ValueError("%s must be a dense [%d] of the type of q" % (name, D))
+    q_out = _new(q.shape, q.dtype, q.device, stream) if q_out is None else q_out
+    if q_out.shape != q.shape or q_out.dtype != q.dtype:
+        raise ValueError("q_out must have the shape and type of q")
+    d = pab_qk_norm(dtype, norm, n // grid, Hq, 0, D, tuple(places), tuple(axis_dim), eps, q.data_ptr(), 0, q_out.data_ptr(), 0,
+                    ld_q, 0, _heads_of(q_out, "q_out")[3], 0, *(0 if t is None else t.data_ptr() for t in (gamma_q, beta_q, gamma_k, beta_k, factors)))
+    if k is not None:
+        m, Hk, Dk, d.ld_k = _heads_of(k, "k")
+        if (m, Dk) != (n, D) or k.dtype != q.dtype:
+            raise ValueError("k must have the tokens, head dim and type of q")
+        k_out = _new(k.shape, k.dtype, k.device, stream) if k_out is None else k_out
+        if k_out.shape != k.shape or k_out.dtype != k.dtype:
+            raise ValueError("k_out must have the shape and type of k")
+        d.heads_k, d.k, d.k_out, d.ld_k_out = Hk, k.data_ptr(), k_out.data_ptr(), _heads_of(k_out, "k_out")[3]
+    _same_device(q, k, q_out, k_out, factors, gamma_q, beta_q, gamma_k, beta_k)
+    _check(lib.pab_qk_norm_rope(ctypes.byref(d), _stream(stream)))
+    return q_out, k_out

@@ -1,0 +1,403 @@
+"""8-bit rows on the GPU: quantiser, read-back, products, MLP and the 8-bit broadcast cache against the fp64 definitions.
+
+Tolerances.  Quantising is exact (a power of two divides exactly, one rounding follows): bytes are compared.  A result rounded to bf16 is at most
+2^-8 of it off; an fp32 sum of n terms at most n 2^-24 of the sum of their magnitudes, in any order.  The matrix instruction for
+8-bit values adds its products by eights of neighbouring columns: within one, products are lined up to the largest exponent (that of the factors'
+exponents together, -6 for a subnormal factor) and lose, towards zero, what lies more than 13 places below (2^15 + 2^2 is exact, 2^15 +
+2^1 gives 2^15; from one group to another and from group to accumulator fp32 holds: 2^15 + 2^-8 is exact).  Seven products may lose less than
+2^-13 of that power of two each, so a group is less than 7 * 2^-13 of it off, and it is at most the product of the group's largest factors."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import q8_oracle as qo
+from paper_2408_12588_amd import pab, workloads as W
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+BF = 2.0 ** -8
+F32 = 2.0 ** -24
+
+
+def rows_of(q8):
+    torch.cuda.synchronize()
+    return q8.data.cpu().numpy().view(np.uint8), q8.scale.cpu().numpy().view(np.uint8)
+
+
+def assert_rows(q8, x, K):
+    """The 8-bit rows are the definition's, byte for byte (a NaN's sign aside)."""
+    data, scale = rows_of(q8)
+    want, ws = qo.quantize(x)
+    nb = qo.blocks(K)
+    assert np.array_equal(scale[:, :nb], ws)
+    got = data[:, :128 * nb]
+    nan = (want & 0x7F) == 0x7F
+    assert np.array_equal(got[~nan], want[~nan]) and np.all((got[nan] & 0x7F) == 0x7F)
+
+
+def normal(seed, *shape):
+    return torch.from_numpy(np.random.Generator(np.random.Philox(seed)).standard_normal(shape, dtype=np.float32))
+
+
+def make_q8(x, ld=0, ld_scale=0):
+    """8-bit rows of a CPU tensor, by the definition, with optional wider pitches (the rest of a row filled with junk)."""
+    data, scale = qo.quantize(x.double().numpy())
+    R, nb = scale.shape
+    d = torch.full((R, max(ld, data.shape[1])), 0x7F, dtype=torch.uint8)
+    s = torch.full((R, max(ld_scale, (nb + 3) // 4 * 4)), 0xFF, dtype=torch.uint8)
+    d[:, :data.shape[1]], s[:, :nb] = torch.from_numpy(data), torch.from_numpy(scale)
+    return pab.Q8(d.to(DEV), s.to(DEV), x.shape[1]), qo.dequantize(data, scale, x.shape[1])
+
+
+# ---- quantise ----
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("rows,K", [(1, 8), (1, 1152), (2, 120), (17, 128), (63, 136), (300, 320), (5, 4608), (1000, 576), (257, 1024)])
+def test_quantize(dtype, rows, K):
+    x = (normal(rows + K, rows, K) * 10.0 ** torch.linspace(-6, 6, rows)[:, None]).to(dtype)
+    assert_rows(pab.pab_quantize(x.to(DEV)), x.double().numpy(), K)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_quantize_special_values(dtype):
+    inf, nan = float("inf"), float("nan")
+    x = torch.zeros(16, 256)
+    x[1, 5] = -0.0
+    for r, k in ((2, -127), (3, -40), (4, 0), (5, 100), (6, 119)):
+        x[r, :128] = 448.0 * 2.0 ** k                       # the largest value that a scale holds ...
+        x[r, 128:] = 452.0 * 2.0 ** k                       # ... and more (both are bf16 numbers)
+    x[7, 3], x[7, 4], x[7, 5], x[7, 6] = inf, -inf, nan, 2.0
+    x[8, :] = nan
+    x[9, 0] = 2.0 ** -133                                    # subnormal magnitudes
+    x[9, 128:] = 2.0 ** -130
+    x[10, :] = 3.3e38
+    x[11, :128] = torch.linspace(0, 448, 128)
+    x[11, 128:] = torch.linspace(-2.0 ** -5, 2.0 ** -5, 128)
+    x[11, 128] = 448.0                                       # everything else below the smallest normal value
+    x[12, :] = -x[11, :]
+    x[13, :] = torch.arange(256) * 1.0625
+    x = x.to(dtype)
+    assert_rows(pab.pab_quantize(x.to(DEV)), x.double().numpy(), 256)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_quantize_pitches_and_neighbours(dtype):
+    """Strided input, wider output pitches: nothing outside the rows is written."""
+    big = normal(5, 20, 3, 200).to(dtype).to(DEV)
+    x = big[:, 1, 24:24 + 136]
+    d = torch.full((22, 512), 0xAB, dtype=torch.uint8, device=DEV)
+    s = torch.full((22, 8), 0xCD, dtype=torch.uint8, device=DEV)
+    out = pab.pab_quantize(x, out=pab.Q8(d[1:21], s[1:21], 136))
+    assert_rows(out, x.cpu().double().numpy(), 136)
+    assert bool((d[0] == 0xAB).all()) and bool((d[21] == 0xAB).all()) and bool((d[:, 256:] == 0xAB).all())
+    assert bool((s[0] == 0xCD).all()) and bool((s[21] == 0xCD).all()) and bool((s[:, 2:] == 0xCD).all())
+
+
+# ---- read back ----
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("rows,K", [(1, 8), (3, 136), (50, 1152), (257, 64)])
+def test_dequantize_is_exact(dtype, rows, K):
+    y, values = make_q8(normal(rows * K, rows, K), ld=2048, ld_scale=32)
+    out = pab.pab_dequantize(y, dtype=dtype)
+    assert out.dtype == dtype and np.array_equal(out.cpu().double().numpy(), values)   # four bits fit either type
+
+
+def test_dequantize_every_byte_and_scale():
+    data = torch.arange(256, dtype=torch.uint8).repeat(2, 1).view(4, 128)
+    data = torch.cat([data] * 64)
+    scale = torch.zeros(256, 4, dtype=torch.uint8)
+    scale[:, 0] = torch.arange(256, dtype=torch.uint8)
+    out = pab.pab_dequantize(pab.Q8(data.to(DEV), scale.to(DEV), 128), dtype=torch.float32).cpu().double().numpy()
+    want = qo.dequantize(data.numpy(), scale.numpy(), 128)
+    with np.errstate(over="ignore"):
+        want = want.astype(np.float32).astype(np.float64)        # past the largest number: infinity; below the smallest: nearest even
+    assert np.array_equal(out, want, equal_nan=True)
+
+
+@pytest.mark.parametrize("dtype,eps", [(torch.bfloat16, BF), (torch.float32, F32)])
+@pytest.mark.parametrize("rows,K", [(1, 8), (3, 136), (200, 1152)])
+@pytest.mark.parametrize("gated", [False, True])
+def test_residual(dtype, eps, rows, K, gated):
+    y, values = make_q8(normal(1, rows, K))
+    base = normal(2, rows, 2, K + 8).to(dtype).to(DEV)
+    x = base[:, 1, :K]                                            # pitched
+    gate = normal(3, K).to(dtype) if gated else None
+    add = values * gate.double().numpy() if gated else values
+    want = x.cpu().double().numpy() + add
+    tol = eps * np.abs(want) + 2 * F32 * (np.abs(add) + np.abs(want))
+    kept = base.clone()
+    out = pab.pab_dequantize(y, x, gate.to(DEV) if gated else None)
+    assert out.shape == x.shape and torch.equal(base, kept)
+    assert np.all(np.abs(out.cpu().double().numpy() - want) <= tol)
+    same = pab.pab_dequantize(y, x, gate.to(DEV) if gated else None, out=x)   # in place
+    assert torch.equal(same, out) and torch.equal(base[:, 0], kept[:, 0]) and torch.equal(base[:, 1, K:], kept[:, 1, K:])
+
+
+# ---- products ----
+def eights(values, scale, K):
+    """Largest magnitude of every eight columns, not below the smallest normal value 2^-6 of its block where it is not zero."""
+    v = np.zeros((len(values), -(-K // 128) * 128))
+    v[:, :K] = np.abs(values)
+    v = v.reshape(len(v), -1, 8).max(-1)
+    least = np.repeat(2.0 ** (scale[:, :qo.blocks(K)].astype(float) - 127 - 6), 16, 1)
+    return np.where(v > 0, np.maximum(v, least), 0.0)
+
+
+def product_tolerance(a, av, b, bv, extra=0.0):
+    """What the matrix instruction may be off: fp32 sums, and the places that it drops inside a group of eight."""
+    K = av.shape[1]
+    lost = 7 * 2.0 ** -13 * (eights(av, rows_of(a)[1], K) @ eights(bv, rows_of(b)[1], K).T)
+    return (K + 4) * F32 * (np.abs(av) @ np.abs(bv).T + extra) + lost
+
+
+SHAPES = [(1, 8, 8), (1, 6912, 1152), (2, 136, 128), (15, 64, 136), (17, 72, 320), (63, 248, 1152), (64, 256, 512), (65, 128, 640), (130, 264, 384),
+          (257, 576, 576), (300, 1152, 4608), (1260, 1728, 576), (497, 3456, 1152), (2100, 1152, 1152), (700, 4608, 256), (5000, 40, 72)]
+
+
+def check_product(M, N, K, act, bias, seed, ld=(0, 0)):
+    x, w = normal(seed, M, K), normal(seed + 1, N, K) / K ** 0.5
+    a, av = make_q8(x, *ld)
+    b, bv = make_q8(w, *ld)
+    bs = normal(seed + 2, N).bfloat16() if bias else None
+    bd = bs.double().numpy() if bias else None
+    want = qo.linear(av, bv, bd, act)
+    sum_tol = product_tolerance(a, av, b, bv, np.abs(bd) if bias else 0.0)
+    if act:   # slope at most 1.13; exp2 and the reciprocal are good to a few units in the last place of x / (1 + e)
+        sum_tol = 1.13 * sum_tol + 2.0 ** -18 * np.abs(qo.linear(av, bv, bd)) + 1e-30
+    return a, b, (bs.to(DEV) if bias else None), want, sum_tol
+
+
+@pytest.mark.parametrize("M,N,K", SHAPES)
+@pytest.mark.parametrize("act,bias", [(False, False), (True, True)])
+def test_linear(M, N, K, act, bias):
+    a, b, bs, want, tol = check_product(M, N, K, act, bias, M + N + K)
+    out = pab.pab_linear_quantized(a, b, bs, act=pab.GELU if act else pab.NONE)
+    assert out.shape == (M, N) and out.dtype == torch.bfloat16
+    assert np.all(np.abs(out.cpu().double().numpy() - want) <= BF * np.abs(want) + tol * (1 + BF))
+
+
+def check_rows_near(q8, want, tol, N):
+    """8-bit rows of sums that are within `tol` of `want`: the scale fits some largest value in reach, elements are one rounding off."""
+    data, scale = rows_of(q8)
+    nb = qo.blocks(N)
+    assert not data[:, N:128 * nb].any()
+    lo, hi = (np.zeros((len(want), nb * 128)) for _ in range(2))
+    lo[:, :N], hi[:, :N] = np.maximum(np.abs(want) - tol, 0), np.abs(want) + tol
+    lo, hi = lo.reshape(-1, nb, 128).max(-1), hi.reshape(-1, nb, 128).max(-1)
+    assert np.all(scale[:, :nb] >= qo.scale_byte(lo)) and np.all(scale[:, :nb] <= qo.scale_byte(hi))
+    s = np.repeat(2.0 ** (scale[:, :nb].astype(float) - 127), 128, 1)[:, :N]
+    got = qo.dequantize(data, scale, N)
+    assert np.all(np.abs(got - want) <= np.maximum(2.0 ** -4 * (np.abs(want) + tol), 2.0 ** -10 * s) + tol)
+
+
+@pytest.mark.parametrize("M,N,K", SHAPES)
+@pytest.mark.parametrize("act,bias", [(False, False), (True, True)])
+def test_linear_into_rows(M, N, K, act, bias):
+    a, b, bs, want, tol = check_product(M, N, K, act, bias, M + N + K + 7)
+    out = pab.pab_linear_quantized(a, b, bs, act=pab.GELU if act else pab.NONE, out=pab.q8_empty(M, N, DEV))
+    check_rows_near(out, want, tol, N)
+
+
+@pytest.mark.parametrize("M,N,K", [(33, 136, 200), (300, 1152, 320), (2100, 600, 1152)])
+def test_linear_pitches_and_neighbours(M, N, K):
+    """Operands with wide pitches whose spare columns hold NaNs, outputs inside larger buffers."""
+    a, b, bs, want, tol = check_product(M, N, K, False, True, 77, ld=(2048, 24))
+    buf = torch.full((M + 2, N + 24), 7.0, dtype=torch.bfloat16, device=DEV)
+    out = pab.pab_linear_quantized(a, b, bs, out=buf[1:M + 1, 8:N + 8])
+    assert np.all(np.abs(out.cpu().double().numpy() - want) <= BF * np.abs(want) + tol * (1 + BF))
+    buf[1:M + 1, 8:N + 8] = 7.0
+    assert bool((buf == 7.0).all())
+    nb = qo.blocks(N)
+    d = torch.full((M + 2, 128 * nb + 128), 0xAB, dtype=torch.uint8, device=DEV)
+    s = torch.full((M + 2, (nb + 3) // 4 * 4 + 4), 0xCD, dtype=torch.uint8, device=DEV)
+    r = pab.pab_linear_quantized(a, b, bs, out=pab.Q8(d[1:M + 1], s[1:M + 1], N))
+    check_rows_near(r, want, tol, N)
+    d[1:M + 1, :128 * nb], s[1:M + 1, :nb] = 0xAB, 0xCD
+    assert bool((d == 0xAB).all()) and bool((s == 0xCD).all())
+
+
+@pytest.mark.parametrize("out8", [False, True])
+@pytest.mark.parametrize("M,N,K", [(40, 256, 384), (2100, 1152, 1152)])
+def test_linear_nan_stays_in_its_row(M, N, K, out8):
+    x = normal(11, M, K)
+    x[5, K - 1] = float("nan")
+    a, _ = make_q8(x)
+    clean = x.clone()
+    clean[5] = 0
+    c, _ = make_q8(clean)
+    b, _ = make_q8(normal(12, N, K) / K ** 0.5)
+    rows = [i for i in range(M) if i != 5]
+    if out8:
+        r, q = (pab.pab_linear_quantized(t, b, out=pab.q8_empty(M, N, DEV)) for t in (a, c))
+        nb = qo.blocks(N)
+        assert torch.equal(r.data[rows], q.data[rows]) and torch.equal(r.scale[rows, :nb], q.scale[rows, :nb])
+        assert bool(((r.data[5, :N] & 0x7F) == 0x7F).all()) and not bool(r.data[5, N:].any())
+    else:
+        r, q = (pab.pab_linear_quantized(t, b) for t in (a, c))
+        assert torch.equal(r[rows], q[rows]) and bool(r[5].isnan().all())
+
+
+def test_linear_scales_of_both_operands():
+    """Every block has another scale, from 2^-60 to 2^60, and their products count."""
+    M, N, K = 70, 200, 1152
+    rng = np.random.default_rng(3)
+    x, w = normal(21, M, K), normal(22, N, K)
+    ex, ew = rng.integers(-30, 31, size=(M, 9)), rng.integers(-30, 31, size=(N, 9))
+    x *= torch.from_numpy(np.repeat(2.0 ** ex, 128, 1)).float()
+    w *= torch.from_numpy(np.repeat(2.0 ** ew, 128, 1)).float()
+    (a, av), (b, bv) = make_q8(x), make_q8(w)
+    want = av @ bv.T
+    tol = BF * np.abs(want) + 1.01 * product_tolerance(a, av, b, bv)
+    out = pab.pab_linear_quantized(a, b)
+    assert np.all(np.abs(out.cpu().double().numpy() - want) <= tol)
+
+
+def test_linear_same_bits_twice_and_on_a_stream():
+    a, b, bs, want, tol = check_product(1260, 1728, 576, True, True, 31)
+    first = pab.pab_linear_quantized(a, b, bs, act=pab.GELU)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    again = [pab.pab_linear_quantized(a, b, bs, act=pab.GELU, stream=side) for _ in range(3)]
+    side.synchronize()
+    assert all(torch.equal(first, t) for t in again)
+
+
+def test_offsets_past_32_bits():
+    """Rows whose byte offsets pass 2^32 in input, 8-bit rows and output."""
+    R, K = (1 << 31) // 1152 + 3000, 1152
+    assert R * K > 1 << 31 and R * K * 2 > 1 << 32
+    x = torch.empty(R, K, dtype=torch.bfloat16, device=DEV)
+    picks = [0, R // 2, (1 << 31) // K, (1 << 31) // K + 1, R - 1]
+    x.fill_(0.0)
+    for i in picks:
+        x[i] = normal(i, K).bfloat16().to(DEV)
+    y = pab.pab_quantize(x)
+    sub = pab.Q8(y.data[picks], y.scale[picks], K)
+    assert_rows(sub, x[picks].cpu().double().numpy(), K)
+    back = pab.pab_dequantize(y, x, out=x)
+    want = qo.dequantize(sub.data.cpu().numpy(), sub.scale.cpu().numpy(), K)
+    got = back[picks].cpu().double().numpy()
+    assert np.all(np.abs(got - 2 * want) <= 2 * BF * np.abs(want) + np.abs(want) * 2.0 ** -3 + 1e-3)
+    w, wv = make_q8(normal(8, 1152, K) / K ** 0.5)
+    c = pab.pab_linear_quantized(y, w, out=x)
+    lin = want @ wv.T
+    tol = product_tolerance(sub, want, w, wv)
+    assert np.all(np.abs(c[picks].cpu().double().numpy() - lin) <= BF * np.abs(lin) + 1.01 * tol)
+
+
+# ---- the MLP ----
+def mlp_case(n, C, F, seed):
+    x = (normal(seed, n, C) * 2 + 0.5).bfloat16()
+    shift, scale = (0.1 * normal(seed + 1, C)).bfloat16(), (0.1 * normal(seed + 2, C)).bfloat16()
+    b1, b2 = normal(seed + 3, F).bfloat16(), normal(seed + 4, C).bfloat16()
+    (w1, v1), (w2, v2) = make_q8(normal(seed + 5, F, C) / C ** 0.5), make_q8(normal(seed + 6, C, F) / F ** 0.5)
+    want = qo.mlp(*(t.double().numpy() for t in (x, shift, scale)), v1, b1.double().numpy(), v2, b2.double().numpy())
+    w = pab.mlp_weights_quantized(shift.to(DEV), scale.to(DEV), w1, b1.to(DEV), w2, b2.to(DEV))
+    return x.to(DEV), w, want
+
+
+@pytest.mark.parametrize("n,C,F", [(1, 32, 32), (3, 160, 96), (130, 576, 2304), (300, 1152, 4608), (1260, 576, 2304), (40, 2048, 4096), (257, 800, 1600)])
+def test_mlp(n, C, F):
+    """Norm of the error.  Rounding the output: 2^-8 / sqrt(3) = 0.0023 of it.  A value next to a border of e4m3 may fall to the other side, a step of
+    at most 2^-3 of it: behind the layernorm, whose fp32 sums are 2^-20 off, one in 10^5 (0.125 * 10^-2.5 = 0.0004 of the norm), behind
+    the first product, whose sums are some 2^-14 off, one in 10^3 (0.125 * 10^-1.5 = 0.0040).  Together 0.0046 of the norm; 2^-8 + 0.0025 = 0.0064."""
+    x, w, want = mlp_case(n, C, F, n + C)
+    got = pab.pab_mlp_compute_quantized(x, w).cpu().double().numpy()
+    assert np.linalg.norm(got - want) <= (BF + 0.0025) * np.linalg.norm(want)
+
+
+def test_mlp_keeps_its_rows():
+    """A token's output does not depend on the others, scratch content does not matter."""
+    x, w, _ = mlp_case(300, 576, 1152, 3)
+    scratch = torch.full((pab.pab_mlp_scratch_bytes_quantized(300, 576, 1152),), 0x7F, dtype=torch.uint8, device=DEV)
+    a = pab.pab_mlp_compute_quantized(x, w, scratch=scratch)
+    y = x.clone()
+    y[7] = float("nan")
+    b = pab.pab_mlp_compute_quantized(y, w, scratch=scratch)
+    rows = [i for i in range(300) if i != 7]
+    assert torch.equal(a[rows], b[rows]) and bool(b[7].isnan().all())
+
+
+# ---- the 8-bit broadcast cache ----
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_attention_slots_are_quantised_outputs(dtype):
+    """Over a whole schedule: the 8-bit slot is the quantised slot of an ordinary context, byte for byte; reuse touches nothing."""
+    wl = W.Workload("q", 2, 3, 40, 12, 4, 72, dtype, 7, (2, 3, 2), 1, 5, seed=5)
+    plain, eight = pab.PabContext(pab.config_of(wl), DEV), pab.QuantizedContext(pab.config_of(wl), DEV)
+    eight.workspace.fill_(0x7F)
+    scratch = torch.empty(wl.tokens * 288 * wl.elem_size, dtype=torch.uint8, device=DEV)
+    C = wl.heads * wl.head_dim
+    for step in range(wl.n_steps):
+        for block, kind in wl.calls_per_step():
+            q, k, v = (t.to(DEV) for t in W.make_qkv(wl, block, kind, step))
+            dec, _ = plain.pab_attention(block, kind, step, q, k, v)
+            if dec == pab.REUSE:
+                before = eight.workspace.clone()
+                got, slot = eight.pab_attention_quantized(block, kind, step, None, None, None, None)
+                assert torch.equal(before, eight.workspace)
+            else:
+                got, slot = eight.pab_attention_quantized(block, kind, step, q, k, v, scratch)
+            assert got == dec
+            want = pab.pab_quantize(plain.slot_tensor(block, kind).view(wl.tokens, C))
+            assert torch.equal(slot.data, want.data) and torch.equal(slot.scale[:, :3], want.scale[:, :3])
+            view = eight.slot_tensor(block, kind)
+            assert view.data.data_ptr() == slot.data.data_ptr() == eight.pab_slot_ptr(block, kind)
+    assert eight.pab_launch_count() == plain.pab_launch_count()
+    eight.pab_reset()
+    with pytest.raises(pab.PabError):
+        eight.pab_attention_quantized(0, 0, 2, None, None, None, None)
+
+
+def test_module_slots_are_quantised_outputs():
+    wl = W.Workload("qm", 1, 4, 30, 20, 4, 72, "bf16", 5, (2, 2, 2), 1, 4, seed=6)
+    cfg = pab.config_of(wl)
+    plain, eight = pab.PabContext(cfg, DEV), pab.QuantizedContext(cfg, DEV)
+    scratch = pab.module_scratch(wl.T, wl.S, wl.L, wl.heads, wl.head_dim, DEV)
+    text = W.make_text(wl).to(DEV)
+    C = wl.heads * wl.head_dim
+    for kind in range(3):
+        w = pab.module_weights(**{n: t.to(DEV) for n, t in W.make_module_weights(wl, 0, kind).items()})
+        for step in range(wl.n_steps):
+            x = W.make_module_input(wl, 0, kind, step).to(DEV)
+            tx = text if kind == W.CROSS else None
+            dec, _ = plain.pab_module_attention(0, kind, step, x, tx, w, scratch)
+            if dec == pab.REUSE:
+                got, slot = eight.pab_module_attention_quantized(0, kind, step, None, None, None, None)
+            else:
+                got, slot = eight.pab_module_attention_quantized(0, kind, step, x, tx, w, scratch)
+            want = pab.pab_quantize(plain.slot_tensor(0, kind).reshape(wl.tokens, C))
+            assert got == dec and torch.equal(slot.data, want.data) and torch.equal(slot.scale[:, :3], want.scale[:, :3])
+
+
+# ---- graphs ----
+def test_captured_calls_follow_their_inputs():
+    """Quantise, product into rows, product, residual and the MLP in a graph: every replay gives what the eager calls give."""
+    n, C, F = 300, 576, 1152
+    x, w, _ = mlp_case(n, C, F, 9)
+    w1, w2 = w._keep[2], w._keep[4]
+    gate = normal(1, C).bfloat16().to(DEV)
+    scratch = torch.empty(pab.pab_mlp_scratch_bytes_quantized(n, C, F), dtype=torch.uint8, device=DEV)
+    q, u, y, out, m = pab.q8_empty(n, C, DEV), pab.q8_empty(n, F, DEV), torch.empty_like(x), torch.empty_like(x), torch.empty_like(x)
+    z = pab.q8_empty(n, C, DEV)
+
+    def chain():
+        pab.pab_quantize(x, out=q)
+        pab.pab_linear_quantized(q, w1, act=pab.GELU, out=u)
+        pab.pab_linear_quantized(u, w2, out=y)
+        pab.pab_quantize(y, out=z)
+        pab.pab_dequantize(z, x, gate, out=out)
+        pab.pab_mlp_compute_quantized(x, w, scratch=scratch, out=m)
+
+    chain()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        chain()
+    for seed in range(4):
+        x.copy_(normal(100 + seed, n, C).bfloat16().to(DEV))
+        graph.replay()
+        torch.cuda.synchronize()
+        replayed = out.clone(), m.clone()
+        out.zero_(), m.zero_()
+        chain()
+        torch.cuda.synchronize()
+        assert torch.equal(replayed[0], out) and torch.equal(replayed[1], m)
