@@ -31,10 +31,10 @@ struct GemmQ8Params {
 
 enum { Q8_NONE = 0, Q8_GELU = 1 };
 
-__device__ __forceinline__ i32x8 lds_read32(unsigned addr) {   // chunks q16 and q16 + 4 of a row
+__device__ __forceinline__ i32x8 lds_read32(unsigned addr, unsigned addr4) {   // chunks q16 and q16 + 4 of a row: addresses 64 ^ apart
   typedef __attribute__((ext_vector_type(4))) int i32x4;
   typedef const __attribute__((address_space(3))) i32x4 *ptr;
-  const i32x4 lo = *(ptr)(size_t)addr, hi = *(ptr)(size_t)(addr ^ 64);
+  const i32x4 lo = *(ptr)(size_t)addr, hi = *(ptr)(size_t)addr4;
   return i32x8{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
 }
 __device__ __forceinline__ int lds_read_byte(unsigned addr) {
@@ -51,6 +51,15 @@ __device__ __forceinline__ void dma4_to_lds(const void *from, unsigned lds_addr)
   asm volatile("s_nop 0\n\tglobal_load_lds_dword %0, off"
                :
                : "v"(from), "{m0}"(lds_addr)
+               : "memory");
+}
+
+// ... from base + voff (base uniform)
+__device__ __forceinline__ void dma4_to_lds(const void *base, unsigned voff, unsigned lds_addr) {
+  lds_addr = __builtin_amdgcn_readfirstlane(lds_addr);
+  asm volatile("s_nop 0\n\tglobal_load_lds_dword %0, %1"
+               :
+               : "v"(voff), "s"(base), "{m0}"(lds_addr)
                : "memory");
 }
 
@@ -157,12 +166,12 @@ __global__ __launch_bounds__(64 * WM * WN * KG, KG > 1 ? WM * WN * KG / 4 : 2) v
 #pragma unroll
     for (int a = 0; a < MS; ++a) {
       ts[a] = lds_read_byte(ss + 4 * (t_row + 16 * a));
-      tf[a] = lds_read32(st + 128 * (t_row + 16 * a) + op);
+      tf[a] = lds_read32(st + 128 * (t_row + 16 * a) + op, st + 128 * (t_row + 16 * a) + (op ^ 64));
     }
 #pragma unroll
     for (int b = 0; b < NS; ++b) {
       ws[b] = lds_read_byte(ss + 4 * (w_row + 16 * b));
-      wf[b] = lds_read32(st + 128 * (w_row + 16 * b) + op);
+      wf[b] = lds_read32(st + 128 * (w_row + 16 * b) + op, st + 128 * (w_row + 16 * b) + (op ^ 64));
     }
 #pragma unroll
     for (int b = 0; b < NS; ++b)

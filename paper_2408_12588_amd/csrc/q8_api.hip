@@ -4,6 +4,7 @@
 #include <cmath>
 
 #include "gemm_q8.hpp"
+#include "gemm_q8_stream.hpp"
 #include "pab_internal.hpp"
 #include "q8_plan.hpp"
 #include "q8_rows.hpp"
@@ -57,8 +58,12 @@ int check_pitch(const char *name, const void *p, long long ld, long long K, int 
 // ---- products ----
 template <int ACT, bool OUT8>
 int launch_product(const pab::GemmPlan &g, const pab::GemmQ8Params &p, hipStream_t st) {
-  const dim3 tiles((unsigned)((g.n_units + 7) / 8 * 8));
+  const dim3 persistent((unsigned)std::min(g.n_units, pab::GEMM_CUS)), tiles((unsigned)((g.n_units + 7) / 8 * 8));
   switch (g.kernel) {
+    case 8: hipLaunchKernelGGL((pab::gemm_q8_stream_kernel<8, 4, ACT, OUT8>), persistent, dim3(512), 0, st, p); break;
+    case 9:
+      if constexpr (!OUT8) hipLaunchKernelGGL((pab::gemm_q8_stream_kernel<9, 3, ACT, false>), persistent, dim3(512), 0, st, p);
+      break;
     case 64:
       if constexpr (!OUT8) hipLaunchKernelGGL((pab::gemm_q8_tile_kernel<2, 2, 2, 2, 3, 1, ACT, false>), tiles, dim3(256), 0, st, p);
       break;

@@ -13,6 +13,8 @@ inline GemmPlan plan_q8(int M, int N, int nk, bool out8) {
     plan_tile(65, 2.95, 0.185, 0.17, 0.55, M, N, nk, &best);
   }
   plan_tile(128, 3.5, 0.55, 0.52, 2.2, M, N, nk, &best);
+  if (!out8 || N % 128 == 0) plan_stream(8, M, N, nk, &best);   // tiles moved back to the edge start at whole blocks
+  if (!out8) plan_stream(9, M, N, nk, &best);
   return best;
 }
 
