@@ -263,7 +263,11 @@ class _NoBinding:
     def attention(*args):
         return NotImplemented
 
-    attention_compute = attention
+    attention_compute = q8_ok = quantize = dequantize = linear_quantized = qk_norm_rope = attention
+
+    @staticmethod
+    def bind_q8(q8_type):
+        pass
 
 
 def _load_binding():
@@ -275,6 +279,8 @@ def _load_binding():
         spec = importlib.util.spec_from_file_location(__package__ + "._binding", path)
         binding = importlib.util.module_from_spec(spec)
         spec.loader.exec_module(binding)
+        if not hasattr(binding, "bind_q8"):
+            raise ImportError("built from an earlier source")
     except ImportError as e:
         warnings.warn("%s does not load: calls go through ctypes (%s)" % (os.path.basename(path), e))
         return _NoBinding
@@ -631,9 +637,12 @@ def _new(shape, dtype, device, stream):
 class Q8:
     """8-bit rows: ``data`` [rows, >= K rounded up to 128] (uint8 or e4m3), ``scale`` [rows, ...] exponent bytes (uint8), device
     tensors that this object keeps; ``K`` columns of values."""
-    __slots__ = ("data", "scale", "K", "struct")
+    __slots__ = ("data", "scale", "K")
 
     def __init__(self, data, scale, K: int):
+        self.data, self.scale, self.K = data, scale, K
+        if _binding.q8_ok(data, scale, K) is True:
+            return
         if data.dim() != 2 or scale.dim() != 2 or data.element_size() != 1 or scale.element_size() != 1:
             raise ValueError("data and scale are matrices of bytes")
         if not data.is_cuda or not scale.is_cuda:
@@ -645,12 +654,24 @@ class Q8:
         nb = (K + 127) // 128
         if K < 1 or data.shape[1] < 128 * nb or scale.shape[1] < nb or data.stride(1) != 1 or scale.stride(1) != 1:
             raise ValueError("K=%d wants dense rows of at least %d bytes and %d scales" % (K, 128 * nb, nb))
-        self.data, self.scale, self.K = data, scale, K
-        self.struct = pab_q8(data.data_ptr(), scale.data_ptr(), data.stride(0), scale.stride(0))
+
+    @property
+    def struct(self) -> pab_q8:
+        return pab_q8(self.data.data_ptr(), self.scale.data_ptr(), self.data.stride(0), self.scale.stride(0))
 
     @property
     def rows(self) -> int:
         return self.data.shape[0]
+
+
+_binding.bind_q8(Q8)
+
+
+def _q8_of(data, scale, K: int) -> Q8:
+    """Rows whose tensors are known to fit."""
+    y = Q8.__new__(Q8)
+    y.data, y.scale, y.K = data, scale, K
+    return y
 
 
 def q8_empty(rows: int, K: int, device="cuda:0", stream=None) -> Q8:
@@ -677,6 +698,10 @@ def _q8_inside(buffer, s: pab_q8, rows: int, K: int) -> Q8:
 
 def pab_quantize(x, out: Q8 | None = None, stream=None) -> Q8:
     """x ``[..., K]`` bf16 or f32 (dense last axis) -> 8-bit rows."""
+    if out is None:
+        done = _binding.quantize(x, stream)
+        if done is not NotImplemented:
+            return _q8_of(*done)
     dtype = _float_type(x, "x")
     rows, K, ldx = _rows_of(x, "x")
     if out is None:
@@ -690,6 +715,9 @@ def pab_quantize(x, out: Q8 | None = None, stream=None) -> Q8:
 
 def pab_dequantize(y: Q8, x=None, gate=None, dtype=None, out=None, stream=None):
     """out = x + gate * y: x ``[..., K]`` or None (0), gate ``[K]`` or None (1); type and shape of x, else ``dtype`` (bf16) and [rows, K]."""
+    done = _binding.dequantize(y, x, gate, dtype, out, stream)
+    if done is not NotImplemented:
+        return done
     if dtype is None:
         dtype = x.dtype if x is not None else out.dtype if out is not None else torch.bfloat16
     ldx = 0
@@ -713,6 +741,9 @@ def pab_dequantize(y: Q8, x=None, gate=None, dtype=None, out=None, stream=None):
 def pab_linear_quantized(a: Q8, w: Q8, bias=None, act: int = NONE, out=None, stream=None):
     """act(a @ w.T + bias) of 8-bit rows a [M, K], w [N, K]; bias ``[N]`` bf16 or None.  ``out``: a bf16 tensor ``[..., N]`` (new if None),
     or a ``Q8`` [M, N] that the result is quantised into."""
+    done = _binding.linear_quantized(a, w, bias, act, out, stream)
+    if done is not NotImplemented:
+        return done
     M, N, K = a.rows, w.rows, a.K
     if w.K != K:
         raise ValueError("a has %d columns, w %d" % (K, w.K))
@@ -854,6 +885,9 @@ def pab_qk_norm_rope(q, k, places, axis_dim, factors=None, norm: int = NORM_LAYE
                      eps: float = 1e-6, q_out=None, k_out=None, stream=None):
     """Norm per head and rotation of q ``[..., Hq, D]`` and k ``[..., Hk, D]`` (or None), tokens in the order of the grid ``places`` (times a
     batch); ``factors`` from pab_rope_factors (None: no rotation).  -> (q_out, k_out); they may be q and k."""
+    done = _binding.qk_norm_rope(q, k, places, axis_dim, factors, norm, gamma_q, beta_q, gamma_k, beta_k, eps, q_out, k_out, stream)
+    if done is not NotImplemented:
+        return done
     n, Hq, D, ld_q = _heads_of(q, "q")
     dtype = _float_type(q, "q")
     grid = places[0] * places[1] * places[2]

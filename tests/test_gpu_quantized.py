@@ -402,3 +402,65 @@ def test_captured_calls_follow_their_inputs():
         chain()
         torch.cuda.synchronize()
         assert torch.equal(replayed[0], out) and torch.equal(replayed[1], m)
+
+
+# ---- the two ways a call is marshalled ----
+def test_native_binding_and_python_agree(monkeypatch):
+    M, N, K = 70, 264, 200
+    x = normal(1, M, 2, K).to(DEV)[:, 1]
+    w = pab.pab_quantize(normal(2, N, K).bfloat16().to(DEV))
+    bias, gate, res = normal(3, N).bfloat16().to(DEV), normal(4, K).to(DEV), normal(5, M, K).to(DEV)
+    q, k = normal(6, 24, 4, 32).to(DEV), normal(7, 24, 2, 32).to(DEV)
+    gamma = normal(8, 32).to(DEV)
+    f = pab.pab_rope_factors((2, 3, 4), (8, 8, 8), device=DEV)
+
+    def calls():
+        a = pab.pab_quantize(x)
+        out = [a.data, a.scale[:, :2], pab.pab_dequantize(a), pab.pab_dequantize(a, dtype=torch.float32), pab.pab_dequantize(a, res, gate),
+               pab.pab_dequantize(a, res), pab.pab_dequantize(a, out=torch.empty(M, K, device=DEV)),
+               pab.pab_linear_quantized(a, w), pab.pab_linear_quantized(a, w, bias, act=pab.GELU),
+               pab.pab_linear_quantized(a, w, bias, out=torch.empty(M, N, device=DEV, dtype=torch.bfloat16))]
+        y = pab.pab_linear_quantized(a, w, bias, out=pab.q8_empty(M, N, DEV))
+        out += [y.data, y.scale[:, :3], *pab.pab_qk_norm_rope(q, k, (2, 3, 4), (8, 8, 8), f, pab.NORM_RMS, gamma, None, None, gamma, eps=1e-5),
+                pab.pab_qk_norm_rope(q, None, (2, 3, 2), (0, 0, 0), None, pab.NORM_LAYER)[0]]
+        return out
+
+    native = calls()
+    assert pab._binding.quantize(x, None) is not NotImplemented
+    monkeypatch.setattr(pab, "_binding", pab._NoBinding)
+    python = calls()
+    assert len(native) == len(python)
+    for a, b in zip(native, python):
+        assert a.dtype == b.dtype and a.shape == b.shape and torch.equal(a, b)
+
+
+@pytest.mark.parametrize("native", [True, False])
+def test_python_refuses_what_does_not_fit(native, monkeypatch):
+    if not native:
+        monkeypatch.setattr(pab, "_binding", pab._NoBinding)
+    x = normal(1, 4, 128).bfloat16().to(DEV)
+    a = pab.pab_quantize(x)
+    w = pab.pab_quantize(normal(2, 16, 128).to(DEV))
+    other = pab.pab_quantize(normal(2, 16, 256).to(DEV))
+    half = torch.zeros(4, 128, device=DEV, dtype=torch.float16)
+    q = normal(3, 6, 2, 32).to(DEV)
+    f = pab.pab_rope_factors((1, 2, 3), (8, 8, 8), device=DEV)
+    bad = [lambda: pab.pab_quantize(half), lambda: pab.pab_quantize(x.t()), lambda: pab.pab_quantize(x, out=w), lambda: pab.pab_quantize(x[:, :4]),
+           lambda: pab.pab_quantize(x[:0]), lambda: pab.pab_quantize(torch.zeros((), device=DEV)),
+           lambda: pab.pab_dequantize(a, x.float(), dtype=torch.bfloat16), lambda: pab.pab_dequantize(a, half), lambda: pab.pab_dequantize(a, x[:3]),
+           lambda: pab.pab_dequantize(a, gate=x[0, :64]), lambda: pab.pab_dequantize(a, gate=x[0].float()), lambda: pab.pab_dequantize(a, out=half),
+           lambda: pab.pab_linear_quantized(a, other), lambda: pab.pab_linear_quantized(a, w, x[0, :8]), lambda: pab.pab_linear_quantized(a, w, act=2),
+           lambda: pab.pab_linear_quantized(a, w, out=x), lambda: pab.pab_linear_quantized(a, w, out=a),
+           lambda: pab.pab_linear_quantized(a, w, out=torch.empty(4, 16, device=DEV)),
+           lambda: pab.Q8(a.data, a.scale, 129), lambda: pab.Q8(a.data[:3], a.scale, 128), lambda: pab.Q8(x, a.scale, 128),
+           lambda: pab.Q8(a.data, a.scale.cpu(), 128), lambda: pab.Q8(a.data, a.scale, 0),
+           lambda: pab.pab_qk_norm_rope(q, None, (1, 2, 2), (8, 8, 8), f), lambda: pab.pab_qk_norm_rope(q, None, (1, 2, 3), (8, 8, 6), f),
+           lambda: pab.pab_qk_norm_rope(q, q[:3], (1, 2, 3), (8, 8, 8), f), lambda: pab.pab_qk_norm_rope(q, q.bfloat16(), (1, 2, 3), (8, 8, 8), f),
+           lambda: pab.pab_qk_norm_rope(q, None, (1, 2, 3), (8, 8, 8), f, 3), lambda: pab.pab_qk_norm_rope(q, None, (1, 2, 3), (8, 8, 8), f, gamma_q=q[0, 0, :16]),
+           lambda: pab.pab_qk_norm_rope(q, None, (1, 2, 3), (8, 8, 8), f, q_out=q.bfloat16()), lambda: pab.pab_qk_norm_rope(q, None, (0, 2, 3), (8, 8, 8), f),
+           lambda: pab.pab_qk_norm_rope(q.half(), None, (1, 2, 3), (8, 8, 8), f), lambda: pab.pab_qk_norm_rope(q[..., :16], None, (1, 2, 3), (8, 8, 0)),
+           lambda: pab.pab_qk_norm_rope(q, None, (1, 2, 3), (8, 8, 8), f, eps=-1.0)]
+    for i, call in enumerate(bad):
+        with pytest.raises((ValueError, pab.PabError)):
+            call()
+            pytest.fail("call %d" % i)
