@@ -126,15 +126,21 @@ int ln_modulate_q8(int n_tok, int C, const void *x, const void *shift, const voi
   return launched();
 }
 
+// Workgroups of a long list of rows.  In bf16 a wavefront has as many values for half the bytes and is bound by its instructions: as many as the chip
+// holds at once (six per CU, 80 registers), which keep gamma and beta unpacked: 25440 tokens, 16 heads of 72, us at 1024 / 1536 / 2048 /
+// 4096 / one row group each: 56.3 / 50.0 / 59.8 / 54.2 / 65.5.  In fp32 nothing is unpacked and more, shorter ones are better: 12720 tokens 52.0 /
+// 51.6 / 52.3 / 49.9 / 49.1, at 8192 49.0.
+template <typename T> constexpr long long QK_WGS = sizeof(T) == 2 ? 256 * 6 : 256 * 32;
+
 template <typename T, int NORM>
 int launch_qk(int D, const pab::QkAxesParams &p, hipStream_t st) {
-  auto grid = [&](int lanes) { return dim3((unsigned)((p.n_row + 4LL * (64 / lanes) - 1) / (4 * (64 / lanes)))); };
+  auto grid = [&](int lanes) { return dim3((unsigned)std::min((p.n_row + 4LL * (64 / lanes) - 1) / (4 * (64 / lanes)), QK_WGS<T>)); };
   switch (D) {
-    case 32: hipLaunchKernelGGL((pab::qk_norm_axes_kernel<T, 4, 1, NORM>), grid(4), dim3(256), 0, st, p); break;
-    case 64: hipLaunchKernelGGL((pab::qk_norm_axes_kernel<T, 8, 1, NORM>), grid(8), dim3(256), 0, st, p); break;
-    case 72: hipLaunchKernelGGL((pab::qk_norm_axes_kernel<T, 3, 3, NORM>), grid(3), dim3(256), 0, st, p); break;
-    case 96: hipLaunchKernelGGL((pab::qk_norm_axes_kernel<T, 4, 3, NORM>), grid(4), dim3(256), 0, st, p); break;
-    default: hipLaunchKernelGGL((pab::qk_norm_axes_kernel<T, 16, 1, NORM>), grid(16), dim3(256), 0, st, p); break;
+    case 32: hipLaunchKernelGGL((pab::qk_norm_axes_kernel<T, 4, NORM>), grid(4), dim3(256), 0, st, p); break;
+    case 64: hipLaunchKernelGGL((pab::qk_norm_axes_kernel<T, 8, NORM>), grid(8), dim3(256), 0, st, p); break;
+    case 72: hipLaunchKernelGGL((pab::qk_norm_axes_kernel<T, 9, NORM>), grid(9), dim3(256), 0, st, p); break;
+    case 96: hipLaunchKernelGGL((pab::qk_norm_axes_kernel<T, 12, NORM>), grid(12), dim3(256), 0, st, p); break;
+    default: hipLaunchKernelGGL((pab::qk_norm_axes_kernel<T, 16, NORM>), grid(16), dim3(256), 0, st, p); break;
   }
   return launched();
 }
@@ -318,7 +324,7 @@ int pab_qk_norm_rope(const pab_qk_norm *d, void *hip_stream) {
     n *= d->places[a];
     if (n > 0x7fffffffLL) return fail(PAB_EINVAL, "too many tokens");
   }
-  if (n * heads > (1LL << 27)) return fail(PAB_EINVAL, "%lld tokens of %d heads are too many for one launch", n, heads);
+  if (n * heads > (1LL << 30)) return fail(PAB_EINVAL, "%lld tokens of %d heads are too many for one launch", n, heads);
   if ((rc = check_pitch("q", d->q, d->ld_q, (long long)d->heads_q * D, d->dtype)) != PAB_OK ||
       (rc = check_pitch("q_out", d->q_out, d->ld_q_out, (long long)d->heads_q * D, d->dtype)) != PAB_OK)
     return rc;
@@ -329,7 +335,7 @@ int pab_qk_norm_rope(const pab_qk_norm *d, void *hip_stream) {
     return fail(PAB_EINVAL, "gamma, beta and factors must be 16-byte aligned");
   pab::QkAxesParams p;
   p.q = d->q; p.q_out = d->q_out; p.ld_q = d->ld_q; p.ld_q_out = d->ld_q_out;
-  p.k = d->heads_k ? d->k : nullptr; p.k_out = d->k_out; p.ld_k = d->ld_k; p.ld_k_out = d->ld_k_out;
+  p.k = d->k; p.k_out = d->k_out; p.ld_k = d->ld_k; p.ld_k_out = d->ld_k_out;
   p.gq = d->gamma_q; p.bq = d->beta_q; p.gk = d->gamma_k; p.bk = d->beta_k;
   p.factors = static_cast<const pab::f32x2 *>(d->factors);
   p.heads_q = d->heads_q; p.heads_k = d->heads_k; p.eps = d->eps;
@@ -340,6 +346,7 @@ int pab_qk_norm_rope(const pab_qk_norm *d, void *hip_stream) {
   p.tokens = pab::divisor((unsigned)(n / d->n_batch));
   p.end_t = d->axis_dim[0] / 2; p.end_y = p.end_t + d->axis_dim[1] / 2; p.end_x = p.end_y + d->axis_dim[2] / 2;
   p.first_y = d->places[0] * (d->axis_dim[0] / 2); p.first_x = p.first_y + d->places[1] * (d->axis_dim[1] / 2);
+  p.whole = d->axis_dim[0] % 8 == 0 && d->axis_dim[1] % 8 == 0 && d->axis_dim[2] % 8 == 0;
   const hipStream_t st = static_cast<hipStream_t>(hip_stream);
   return d->dtype == PAB_BF16 ? launch_qk_norm_axes<pab::bf16_t>(d->norm, D, p, st) : launch_qk_norm_axes<float>(d->norm, D, p, st);
 }

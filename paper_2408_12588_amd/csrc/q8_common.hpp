@@ -55,18 +55,18 @@ __device__ __forceinline__ unsigned max16(unsigned v) {
   return max(v, (unsigned)__builtin_amdgcn_mov_dpp((int)v, 0x140, 0xF, 0xF, true));   // mirrored in the row: the other eight
 }
 
-// n / d by a high product: m = 2^64 / d rounded up is off by less than 1, n < 2^32 keeps the quotient exact
+// n / d for n < 2^31 by a high product: with 2^k <= d < 2^(k+1) and m = 2^(32+k) / d rounded up, m is off by less than d / 2^(32+k) of the
+// quotient per unit of n, n d <= 2^(32+k) keeps it exact, and m fits 32 bits unless d is a power of two (then half of both; d = 1: n itself)
 struct Divisor {
-  unsigned d;
-  unsigned long long m;
+  unsigned d, m, k, one;
 };
-inline Divisor divisor(unsigned d) { return {d, d > 1 ? ~0ULL / d + 1 : 0ULL}; }
-__device__ __forceinline__ unsigned quotient(unsigned n, const Divisor &v) {
-  if (v.d == 1) return n;
-  const unsigned long long lo = (unsigned long long)(unsigned)v.m * n;
-  const unsigned long long hi = (v.m >> 32) * n + (lo >> 32);
-  return (unsigned)(hi >> 32);
+inline Divisor divisor(unsigned d) {
+  if (d <= 1) return {1, 0, 0, ~0u};
+  unsigned k = 31 - __builtin_clz(d);
+  if ((d & (d - 1)) == 0) return {d, 0x80000000u, k - 1, 0};
+  return {d, (unsigned)(((1ULL << (32 + k)) + d - 1) / d), k, 0};
 }
+__device__ __forceinline__ unsigned quotient(unsigned n, const Divisor &v) { return (__umulhi(n, v.m) + (n & v.one)) >> v.k; }
 
 // eight values of a row from memory, as fp32, and back
 __device__ __forceinline__ void load_row8(const bf16_t *p, float (&v)[8]) {
