@@ -1,13 +1,15 @@
-// Products of 8-bit rows that fill the chip: one persistent workgroup of 8 wavefronts per CU works through tiles of 256 tokens x 32 NS features,
-// 4 wavefronts along the tokens x 2 along the features, 4 x NS sub-tiles each (layouts and the instruction: gemm_q8.hpp).  The
+// Products of 8-bit rows that fill the chip: one persistent workgroup of 4 wavefronts per CU works through tiles of 256 tokens x 32 NS features,
+// 2 wavefronts along the tokens x 2 along the features, 8 x NS sub-tiles each (layouts and the instruction: gemm_q8.hpp).  The
 // division of the work, the stream of copies through two LDS stages across tile borders, the tail tiles and the tiles moved back to end at
 // the matrix edge (rows that two tiles compute are written twice with the same bits) are those of gemm_stream.hpp; a slice of
 // 128 bytes is twice its multiply-adds.
 //
-// Inside a slice: NS steps of one weight sub-tile (32 bytes a lane, one instruction deep) x the token sub-tiles.  Weight operands are read
-// RING - 1 steps ahead.  Token operands, 8 registers each, have no second set: the last step reads the next slice's behind each
-// product that used the old one.  One barrier per slice, RING - 1 steps before its end, when everything of it has been read: it frees its
-// stage and publishes the other, and the copies of the slice after that go out two per step, so that they have half a slice to arrive.
+// One wavefront per SIMD with all 512 registers (256 or 288 of sums) reads half the operands from LDS that eight wavefronts of half its tile
+// read, and waits for nobody but the copies.  To keep the matrix core fed by itself, it goes through a slice in an order that
+// leaves every load time: weight sub-tiles 0 .. NS - 3 one after the other, each with all token sub-tiles, operands two steps (16
+// products) ahead; then the barrier, when everything of the slice has been read: it frees its stage and publishes the other; then
+// token by token with the last two weight sub-tiles, after which the token's registers take the next slice's operand.  The
+// copies of the slice after that go out one by one between the products behind the barrier.
 // There is no branch inside a slice: the compiler sinks products past one, and then holds their operands.  The copies of a tile of fewer than 256
 // tokens repeat its last rows, and those behind the last tile repeat that tile; nobody reads either.
 #pragma once
@@ -15,8 +17,8 @@
 
 namespace pab {
 
-template <int NS, int RING, int ACT, bool OUT8>
-__global__ __launch_bounds__(512, 2) void gemm_q8_stream_kernel(const GemmQ8Params p) {
+template <int NS, int ACT, bool OUT8>
+__global__ __launch_bounds__(256, 1) void gemm_q8_stream_kernel(const GemmQ8Params p) {
   constexpr int BM = 256, BN = 32 * NS, ROWS = BM + BN;
   // bytes: token rows, pair rows of the weights, odd sub-tiles; a dword of scales for each (copied by 64)
   constexpr int STAGE = 128 * ROWS + 4 * ((ROWS + 63) / 64 * 64);
@@ -24,15 +26,12 @@ __global__ __launch_bounds__(512, 2) void gemm_q8_stream_kernel(const GemmQ8Para
   constexpr bool ODD = NS % 2 != 0;
   constexpr int W0 = 128 * BM, W1 = W0 + 128 * 64 * NPAIR, SC = 128 * ROWS;   // byte offsets in a stage
   constexpr int SHIFT1 = ODD ? 16 : 0;           // features of wave column 1 before its pairs
-  constexpr int NDMA = 4 + NPAIR + (ODD ? 1 : 0);   // copy rounds of a wavefront per slice (the last: wavefronts 0-3)
-  constexpr int AHEAD = RING - 1, JB = NS - AHEAD;  // operand distance, barrier step
-  constexpr int PER = 2;                         // copy rounds per step
-  static_assert(NPAIR % 2 == 0, "pairs are stored two at a time");
-  static_assert(NS % RING == 0 && NDMA <= PER * NS, "the operand ring continues across slices");
+  constexpr int NDMA = 8 + 2 * NPAIR + (ODD ? 1 : 0) + 1;   // copies of a wavefront per slice: 32 rows each, and the scales
+  static_assert(NPAIR == 4, "scales are copied by two pairs, outputs stored by two pairs");
   static_assert(!OUT8 || NS == 8, "a wavefront's features are one block");
   constexpr int BIAS = 2 * STAGE, XPOSE = BIAS + 2048;   // byte offsets: two bias rows, 2 KB per wavefront
 
-  __shared__ __attribute__((aligned(16))) unsigned char smem[XPOSE + 8 * 2048];
+  __shared__ __attribute__((aligned(16))) unsigned char smem[XPOSE + 4 * 2048];
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int l16 = lane & 15, q16 = lane >> 4;
@@ -64,49 +63,55 @@ __global__ __launch_bounds__(512, 2) void gemm_q8_stream_kernel(const GemmQ8Para
   const int wg = gridDim.x == 256 ? (blockIdx.x & 7) * 32 + (blockIdx.x >> 3) : blockIdx.x;
   const int n_mine = (p.n_units - wg + (int)gridDim.x - 1) / (int)gridDim.x;
 
-  // ---- copies: wavefront w moves rows 8 w .. 8 w + 7 of every 64 rows; its lane row lane >> 3, position lane & 7 ----
+  // ---- copies: wavefront w moves rows 8 w .. 8 w + 7 of every 32 rows; its lane row lane >> 3, position lane & 7.  Weight rows lie by
+  //      wave column, pair, sub-tile, operand row; row i of a pair is its feature 8 ((i & 15) >> 2) + 4 (i >> 4) + (i & 3) ----
   const int crow = 8 * wave + (lane >> 3);
   const int cq = (lane & 7) ^ gemm_swizzle(crow);
-  // row i of a round of pair rows, 32 of each wave column: sub-tile (i >> 4) & 1, operand row i & 15
-  auto pair_feature = [](int i) { return (i >> 5) * (16 * NS + SHIFT1) + 8 * ((i & 15) >> 2) + 4 * ((i >> 4) & 1) + (i & 3); };
+  auto in_pair = [](int i) { return 8 * ((i & 15) >> 2) + 4 * (i >> 4) + (i & 3); };
+  constexpr int COL1 = 16 * NS + SHIFT1;         // first paired feature of wave column 1
   // odd sub-tiles: the last 16 features of wave column 0, the first 16 of column 1
   auto odd_feature = [](int i) { return (i >> 4 ? 16 * NS : 32 * NPAIR) + (i & 15); };
-  const unsigned voff_a = (unsigned)(crow * p.lda + 16 * cq), voff_w = (unsigned)(pair_feature(crow) * p.ldw + 16 * cq),
-                 voff_s = (unsigned)(odd_feature(crow & 31) * p.ldw + 16 * cq);
-  // scales: wavefronts 0-3 those of 64 tokens each, 4-7 of a round of pair rows each, 0 the odd rows besides
-  const bool tok_wave = wave < 4;
-  const unsigned soff = (unsigned)(tok_wave ? lane * p.lsa : pair_feature(lane) * p.lsw), soff_s = (unsigned)(odd_feature(lane & 31) * p.lsw);
+  const unsigned voff_a = (unsigned)(crow * p.lda + 16 * cq), voff_w = (unsigned)(in_pair(crow) * p.ldw + 16 * cq),
+                 voff_s = (unsigned)(odd_feature(crow) * p.ldw + 16 * cq);
+  // scales: wavefront w those of 64 tokens and of two pairs, and all of them (the same) those of the odd rows
+  const unsigned soff_a = (unsigned)(lane * p.lsa), soff_w = (unsigned)((32 * (lane >> 5) + in_pair(lane & 31)) * p.lsw),
+                 soff_s = (unsigned)(odd_feature(lane & 31) * p.lsw);
   struct Source {                                // where a tile's slices come from
-    const unsigned char *a, *w, *sc, *so;
-    int last;                                    // last of its rounds of 64 tokens
+    const unsigned char *a, *w, *sa, *sw, *so;
+    int last;                                    // last of its rounds of 32 tokens
   };
   auto source = [&](int i) __attribute__((always_inline)) {
     const Tile t = unit(wg + i * (int)gridDim.x);
     Source s;
-    s.last = t.ms - 1;
+    s.last = 2 * t.ms - 1;
     s.a = p.A + t.m0 * p.lda;
     s.w = p.W + t.n0 * p.ldw;
     s.so = p.sw + t.n0 * p.lsw;
-    s.sc = tok_wave ? p.sa + (t.m0 + 64 * min(wave, s.last)) * p.lsa : s.so + 32 * (wave - 4) * p.lsw;
+    s.sa = p.sa + (t.m0 + 64 * min(wave, t.ms - 1)) * p.lsa;
+    s.sw = s.so + ((wave >> 1) * COL1 + 64 * (wave & 1)) * p.lsw;
     return s;
   };
-  auto copy_round = [&](const Source &s, int kt, int stage, int i) __attribute__((always_inline)) {   // round i of slice kt
+  auto copy_round = [&](const Source &s, int kt, int stage, int i) __attribute__((always_inline)) {   // copy i of slice kt
     const unsigned lds = lds0 + STAGE * stage + 1024 * wave;
-    if (i < 4) dma16_to_lds(s.a + 128LL * kt + 64LL * min(i, s.last) * p.lda, voff_a, lds + 8192 * i);
-    else if (i < 4 + NPAIR) dma16_to_lds(s.w + 128LL * kt + 32LL * (i - 4) * p.ldw, voff_w, lds + W0 + 8192 * (i - 4));
-    else dma16_to_lds(s.w + 128LL * kt, voff_s, lds0 + STAGE * stage + W1 + 1024 * (wave & 3));   // wavefronts 4-7: the same once more
-  };
-  auto copy_scales = [&](const Source &s, int kt, int stage) __attribute__((always_inline)) {
-    const unsigned lds = lds0 + STAGE * stage + SC;
-    dma4_to_lds(s.sc + (kt & ~3), soff, lds + 256 * wave);
-    if (ODD) dma4_to_lds(s.so + (kt & ~3), soff_s, lds + 4 * (BM + 64 * NPAIR));   // all the same
+    if (i == 0) {
+      const unsigned sc = lds0 + STAGE * stage + SC;
+      const int k = kt & ~3;
+      dma4_to_lds(s.sa + k, soff_a, sc + 256 * wave);
+      dma4_to_lds(s.sw + k, soff_w, sc + 4 * BM + 256 * wave);
+      if (ODD) dma4_to_lds(s.so + k, soff_s, sc + 4 * (BM + 64 * NPAIR));
+      return;
+    }
+    --i;
+    if (i < 8) dma16_to_lds(s.a + 128LL * kt + 32LL * min(i, s.last) * p.lda, voff_a, lds + 4096 * i);
+    else if (i < 8 + 2 * NPAIR)
+      dma16_to_lds(s.w + 128LL * kt + ((i - 8) / NPAIR * COL1 + 32 * ((i - 8) % NPAIR)) * p.ldw, voff_w, lds + W0 + 4096 * (i - 8));
+    else dma16_to_lds(s.w + 128LL * kt, voff_s, lds + W1);
   };
 
   Source cur = source(0), nxt = cur;
   for (int stage = 0; stage < 2; ++stage) {      // the first two slices (there are two or more)
 #pragma unroll
     for (int i = 0; i < NDMA; ++i) copy_round(cur, stage, stage, i);
-    copy_scales(cur, stage, stage);
   }
   asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
 
@@ -115,35 +120,36 @@ __global__ __launch_bounds__(512, 2) void gemm_q8_stream_kernel(const GemmQ8Para
   int stage = 0;
 
   auto run_tile = [&](auto ms_tag, const Tile t, int parity) __attribute__((always_inline)) {
-    constexpr int MS = decltype(ms_tag)::value;            // token sub-tiles of a wavefront
+    constexpr int MS = 2 * decltype(ms_tag)::value;        // token sub-tiles of a wavefront
+    constexpr int LAST = NS - 2;                           // the last two weight sub-tiles go token by token
     f32x4 acc[MS][NS];
-    i32x8 tf[MS], wf[RING];                                // token operands, ring of weight operands
-    int ts[MS], ws[RING];                                  // their scales
+    i32x8 tf[MS], wf[3], hf[2];                            // tokens, ring of weights, last two weights
+    int ts[MS], tn[MS], ws[3], hs[2];                      // their scales; tn: the next slice's
     unsigned tb, tb4, wb, wb4, tsb, wsb;
     auto use_stage = [&](int s, int k) __attribute__((always_inline)) {
       const unsigned st = lds0 + STAGE * s;
       tb = st + 2048 * MS * wm + op;
-      wb = st + W0 + 4096 * wn + op;
+      wb = st + W0 + 4096 * NPAIR * wn + op;
       tb4 = tb ^ 64;
       wb4 = wb ^ 64;
       tsb = st + SC + 4 * (16 * MS * wm + l16) + (k & 3);
-      wsb = st + SC + 4 * (BM + 32 * wn + l16) + (k & 3);
+      wsb = st + SC + 4 * (BM + 32 * NPAIR * wn + l16) + (k & 3);
     };
-    auto rd_t = [&](int a) __attribute__((always_inline)) {
-      ts[a] = lds_read_byte(tsb + 64 * a);
-      tf[a] = lds_read32(tb + 2048 * a, tb4 + 2048 * a);
-    };
-    auto rd_w = [&](int b, int slot) __attribute__((always_inline)) {
+    auto rd_t = [&](int a) __attribute__((always_inline)) { tf[a] = lds_read32(tb + 2048 * a, tb4 + 2048 * a); };
+    auto rd_w = [&](int b, i32x8 &w, int &scale) __attribute__((always_inline)) {
       const bool pair = b < 2 * NPAIR;
-      ws[slot] = lds_read_byte(wsb + (pair ? 256 * (b >> 1) + 64 * (b & 1) : 4 * (64 * NPAIR) - 64 * wn));
-      const unsigned off = pair ? 8192 * (b >> 1) + 2048 * (b & 1) : W1 - W0 - 2048 * wn;
-      wf[slot] = lds_read32(wb + off, wb4 + off);
+      scale = lds_read_byte(wsb + (pair ? 64 * b : 4 * 64 * NPAIR - 4 * (32 * NPAIR - 16) * wn));
+      const unsigned off = pair ? 2048 * b : W1 - W0 - (4096 * NPAIR - 2048) * wn;
+      w = lds_read32(wb + off, wb4 + off);
     };
     use_stage(stage, 0);
 #pragma unroll
-    for (int a = 0; a < MS; ++a) rd_t(a);
-#pragma unroll
-    for (int j = 0; j < AHEAD; ++j) rd_w(j, j);
+    for (int a = 0; a < MS; ++a) {
+      ts[a] = lds_read_byte(tsb + 64 * a);
+      rd_t(a);
+    }
+    rd_w(0, wf[0], ws[0]);
+    rd_w(1, wf[1], ws[1]);
 #pragma unroll
     for (int a = 0; a < MS; ++a)
 #pragma unroll
@@ -151,35 +157,51 @@ __global__ __launch_bounds__(512, 2) void gemm_q8_stream_kernel(const GemmQ8Para
 #pragma unroll
         for (int e = 0; e < 4; ++e) acc[a][b][e] = 0.0f;
 
+    // the copies of slice kt + 2: PER behind the barrier of slice kt with every token sub-tile, the others in the first part of slice
+    // kt + 1, every EACH products
+    constexpr int PER = MS == 8 ? 1 : MS == 2 ? 4 : 2, EACH = MS == 8 ? 2 : 1;
+    static_assert(PER * MS + LAST * MS / EACH >= NDMA, "all copies have a place");
     for (int kt = 0; kt < nk; ++kt) {
+      const bool last = kt + 1 >= nk;
+      const Source &before = last ? nxt : cur;
+      const int k1 = last ? 0 : kt + 1;
 #pragma unroll
-      for (int j = 0; j < NS; ++j) {
-        if (j == JB) {   // this slice has been read, the next one has arrived
-          asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-          stage ^= 1;
-          use_stage(stage, kt + 1 == nk ? 0 : kt + 1);
-        }
-        // steps since the barrier; slice kt + 2 (from the barrier on: of this slice, until it: of the last one) goes into the free stage
-        const int d = (j - JB + NS) % NS, ks = kt + (j >= JB ? 2 : 1);
-        const bool over = ks >= nk;
-        const Source &from = over ? nxt : cur;
-        const int k = over ? ks - nk : ks;
-        if (d == 0) copy_scales(from, k, stage ^ 1);
-#pragma unroll
-        for (int r = PER * d; r < PER * d + PER; ++r)
-          if (r < NDMA) copy_round(from, k, stage ^ 1, r);
-        rd_w((j + AHEAD) % NS, (j + AHEAD) % RING);
+      for (int j = 0; j < LAST; ++j) {
+        if (j + 2 < LAST) rd_w(j + 2, wf[(j + 2) % 3], ws[(j + 2) % 3]);
+        else rd_w(j + 2, hf[j + 2 - LAST], hs[j + 2 - LAST]);
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int a = 0; a < MS; ++a) {
-          acc[a][j] = mfma_q8(wf[j % RING], tf[a], acc[a][j], ws[j % RING], ts[a]);
-          if (j == NS - 1) {
-            __builtin_amdgcn_sched_barrier(0);   // not before the product that reads the registers
-            rd_t(a);
-            __builtin_amdgcn_sched_barrier(0);
-          }
+          const int i = PER * MS + (j * MS + a) / EACH;
+          if ((j * MS + a) % EACH == 0 && i < NDMA) copy_round(before, k1, stage ^ 1, i);
+          acc[a][j] = mfma_q8(wf[j % 3], tf[a], acc[a][j], ws[j % 3], ts[a]);
+          __builtin_amdgcn_sched_barrier(0);
         }
+      }
+      asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");   // this slice has been read, the next one has arrived
+      stage ^= 1;
+      use_stage(stage, kt + 1 == nk ? 0 : kt + 1);
+      const int ks = kt + 2;
+      const bool over = ks >= nk;
+      const Source &from = over ? nxt : cur;
+      const int k = over ? ks - nk : ks;
+#pragma unroll
+      for (int a = 0; a < MS; ++a) {
+#pragma unroll
+        for (int i = PER * a; i < PER * a + PER; ++i)
+          if (i < NDMA) copy_round(from, k, stage ^ 1, i);
+        acc[a][LAST] = mfma_q8(hf[0], tf[a], acc[a][LAST], hs[0], ts[a]);
+        __builtin_amdgcn_sched_barrier(0);
+        if (a == 0) rd_w(0, wf[0], ws[0]);
+        if (a == 1) rd_w(1, wf[1], ws[1]);
+        tn[a] = lds_read_byte(tsb + 64 * a);
+        acc[a][LAST + 1] = mfma_q8(hf[1], tf[a], acc[a][LAST + 1], hs[1], ts[a]);
+        __builtin_amdgcn_sched_barrier(0);
+        rd_t(a);
         __builtin_amdgcn_sched_barrier(0);
       }
+#pragma unroll
+      for (int a = 0; a < MS; ++a) ts[a] = tn[a];
     }
 
     const int shift = wn ? SHIFT1 : 0, odd = wn ? 0 : 32 * NPAIR;   // where the pairs / the odd sub-tile start
@@ -268,19 +290,20 @@ __global__ __launch_bounds__(512, 2) void gemm_q8_stream_kernel(const GemmQ8Para
         if (p.bias) b4 = *reinterpret_cast<const bf16x4 *>(bs + odd + 4 * q16);
         bf16_t *dst = p.C + f0 + odd + 8 * (lane & 1) + (long long)(m0 + (lane >> 1)) * p.ldc;
 #pragma unroll
-        for (int a = 0; a < MS; ++a) {
-          bf16x4 y;
+        for (int a0 = 0; a0 < MS; a0 += 4) {               // four sub-tiles are the wavefront's 2 KB
 #pragma unroll
-          for (int e = 0; e < 4; ++e) y[e] = (bf16_t)finish(acc[a][NS - 1][e] + (float)b4[e]);
-          lds_write4(xs + 32 * (16 * a + l16) + 8 * q16, y);
-        }
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+          for (int a = a0; a < MS && a < a0 + 4; ++a) {
+            bf16x4 y;
 #pragma unroll
-        for (int a = 0; a < (MS + 1) / 2; ++a) {
-          const bf16x8 r = lds_read8(xs + 1024 * a + 16 * lane);
-          if (2 * a + 1 < MS || lane < 32) *reinterpret_cast<bf16x8 *>(dst + 32 * a * p.ldc) = r;
+            for (int e = 0; e < 4; ++e) y[e] = (bf16_t)finish(acc[a][NS - 1][e] + (float)b4[e]);
+            lds_write4(xs + 32 * (16 * (a - a0) + l16) + 8 * q16, y);
+          }
+          __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+#pragma unroll
+          for (int a = 0; a < (MS - a0 < 4 ? MS - a0 : 4) / 2; ++a)
+            *reinterpret_cast<bf16x8 *>(dst + (16 * a0 + 32 * a) * p.ldc) = lds_read8(xs + 1024 * a + 16 * lane);
+          __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         }
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
       }
     }
   };
@@ -288,7 +311,7 @@ __global__ __launch_bounds__(512, 2) void gemm_q8_stream_kernel(const GemmQ8Para
   for (int i = 0; i < n_mine; ++i) {
     const Tile t = unit(wg + i * (int)gridDim.x);
     nxt = source(min(i + 1, n_mine - 1));
-    if (p.bias && wave == 7) dma16_to_lds(p.bias + t.n0, 16 * min(lane, BN / 8 - 1), lds0 + BIAS + 1024 * (i & 1));
+    if (p.bias && wave == 3) dma16_to_lds(p.bias + t.n0, 16 * min(lane, BN / 8 - 1), lds0 + BIAS + 1024 * (i & 1));
     if (t.ms == 4) run_tile(std::integral_constant<int, 4>{}, t, i & 1);
     else if (t.ms == 3) run_tile(std::integral_constant<int, 3>{}, t, i & 1);
     else if (t.ms == 2) run_tile(std::integral_constant<int, 2>{}, t, i & 1);

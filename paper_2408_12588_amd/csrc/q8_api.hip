@@ -60,9 +60,9 @@ template <int ACT, bool OUT8>
 int launch_product(const pab::GemmPlan &g, const pab::GemmQ8Params &p, hipStream_t st) {
   const dim3 persistent((unsigned)std::min(g.n_units, pab::GEMM_CUS)), tiles((unsigned)((g.n_units + 7) / 8 * 8));
   switch (g.kernel) {
-    case 8: hipLaunchKernelGGL((pab::gemm_q8_stream_kernel<8, 4, ACT, OUT8>), persistent, dim3(512), 0, st, p); break;
+    case 8: hipLaunchKernelGGL((pab::gemm_q8_stream_kernel<8, ACT, OUT8>), persistent, dim3(256), 0, st, p); break;
     case 9:
-      if constexpr (!OUT8) hipLaunchKernelGGL((pab::gemm_q8_stream_kernel<9, 3, ACT, false>), persistent, dim3(512), 0, st, p);
+      if constexpr (!OUT8) hipLaunchKernelGGL((pab::gemm_q8_stream_kernel<9, ACT, false>), persistent, dim3(256), 0, st, p);
       break;
     case 64:
       if constexpr (!OUT8) hipLaunchKernelGGL((pab::gemm_q8_tile_kernel<2, 2, 2, 2, 3, 1, ACT, false>), tiles, dim3(256), 0, st, p);
