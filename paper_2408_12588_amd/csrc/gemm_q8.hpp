@@ -71,6 +71,36 @@ __device__ __forceinline__ unsigned max_across(unsigned x) {
   return max(b[0], b[1]);
 }
 
+// The largest finite magnitude among a lane's values, as bits, and infinities become NaN: maxima of three without a look at each value (they
+// pass over NaNs), and only where that comes out infinite somewhere in the wavefront value by value.
+template <int N>
+__device__ __forceinline__ unsigned block_max(float (&x)[N][8]) {
+  float m = 0.0f;
+#pragma unroll
+  for (int u = 0; u < N; ++u)
+#pragma unroll
+    for (int e = 0; e < 8; e += 2) m = fmaxf(fmaxf(m, fabsf(x[u][e])), fabsf(x[u][e + 1]));
+  unsigned big = __float_as_uint(m);
+  if (__any(big >= 0x7f800000u)) {
+    big = 0;
+#pragma unroll
+    for (int u = 0; u < N; ++u)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        big = max(big, finite_bits(x[u][e]));
+        x[u][e] = q8_scaled(x[u][e], 1.0f);
+      }
+  }
+  return big;
+}
+
+// GELU in its tanh form, x / (1 + exp(-2 u)), u = sqrt(2 / pi) (x + 0.044715 x^3) (products written out: the same bits wherever it is inlined)
+__device__ __forceinline__ float gelu_q8(float x) {
+#pragma clang fp contract(off)
+  const float s = __builtin_fmaf(x * x, -0.102943236f, -2.302208198f);   // -2 sqrt(2 / pi) log2(e) (0.044715 x^2 + 1)
+  return x * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(x * s));
+}
+
 // ---- everything that does not fill the chip with large tiles: one workgroup per tile, WM x WN wavefronts of MS x NS sub-tiles, K slices
 //      through a ring of NST stages; KG groups of such wavefronts take every KG-th slice through rings of their own, their sums
 //      are added through LDS.  OUT8: a tile's features are whole blocks of 128. ----
@@ -79,10 +109,10 @@ __global__ __launch_bounds__(64 * WM * WN * KG, KG > 1 ? WM * WN * KG / 4 : 2) v
   constexpr int NW = WM * WN, BM = 16 * MS * WM, BN = 16 * NS * WN;
   constexpr int ROWS = BM + BN, STAGE = 132 * ROWS;      // bytes: rows, then a dword of scales for each
   constexpr int ROUNDS = ROWS / 8, MYR = ROUNDS / NW, TOKR = BM / 8 / NW;   // copy rounds: all, per wavefront, of token rows
-  constexpr int SPW = ROWS / NW;                         // scale dwords a wavefront copies
-  static_assert(ROUNDS % NW == 0 && (BM / 8) % NW == 0 && ROWS % NW == 0 && SPW <= 64, "copies must deal evenly to the wavefronts");
+  constexpr int SPW = ROWS / NW, SCN = (SPW + 63) / 64;  // scale dwords a wavefront copies, in copies of 64
+  static_assert(ROUNDS % NW == 0 && (BM / 8) % NW == 0 && ROWS % NW == 0, "copies must deal evenly to the wavefronts");
   static_assert(NS % 2 == 0 && (NS == 2 || NS % 4 == 0) && STAGE % 16 == 0, "sub-tiles come in pairs");
-  static_assert(NST >= 2 && NST <= 3 && (NST - 2) * (MYR + 1) < 16, "vmcnt immediates");
+  static_assert(NST >= 2 && NST <= 3 && (NST - 2) * (MYR + SCN) < 16, "vmcnt immediates");
   constexpr int PART = 1024 * MS * NS * NW;              // bytes of a group's sums
   constexpr int MAXIMA = OUT8 ? 4 * BM * WN : 0;         // a token's largest magnitude, by wavefront column
   static_assert(NW * 2048 + MAXIMA + (KG - 1) * PART <= KG * NST * STAGE, "output staging must fit the rings");
@@ -116,12 +146,18 @@ __global__ __launch_bounds__(64 * WM * WN * KG, KG > 1 ? WM * WN * KG / 4 : 2) v
   for (int i = 0; i < MYR; ++i)
     voff[i] = (unsigned)(source(8 * (wave + NW * i) + (lane >> 3)) * (i < TOKR ? p.lda : p.ldw) + 16 * cq);
   // scales: wavefront w copies those of stage rows SPW w .. SPW w + SPW - 1
-  const int srow = SPW * wave + (lane < SPW ? lane : 0);
-  const unsigned char *scales = srow < BM ? p.sa + (m0 + source(srow)) * p.lsa : p.sw + (n0 + source(srow)) * p.lsw;
+  const unsigned char *scales[SCN];
+#pragma unroll
+  for (int c = 0; c < SCN; ++c) {
+    const int row = SPW * wave + min(64 * c + lane, SPW - 1);
+    scales[c] = row < BM ? p.sa + (m0 + source(row)) * p.lsa : p.sw + (n0 + source(row)) * p.lsw;
+  }
   auto issue = [&](int kt, int stage) __attribute__((always_inline)) {
     const int k = __builtin_amdgcn_readfirstlane(kt);
     const unsigned to = lds0 + STAGE * stage;
-    if (lane < SPW) dma4_to_lds(scales + (k & ~3), to + 128 * ROWS + 4 * SPW * wave);
+#pragma unroll
+    for (int c = 0; c < SCN; ++c)
+      if (64 * c + lane < SPW) dma4_to_lds(scales[c] + (k & ~3), to + 128 * ROWS + 4 * (SPW * wave + 64 * c));
 #pragma unroll
     for (int i = 0; i < MYR; ++i) dma16_to_lds((i < TOKR ? A : W) + 128LL * k, voff[i], to + 1024 * (wave + NW * i));
   };
@@ -150,7 +186,7 @@ __global__ __launch_bounds__(64 * WM * WN * KG, KG > 1 ? WM * WN * KG / 4 : 2) v
   int stage = 0, next = npre % NST;
   for (int s = 0; s < n_step; ++s) {
     // slice s of the group has landed (this wavefront's share); one more may be in flight
-    if (NST == 3 && s + 1 < n_mine) __builtin_amdgcn_s_waitcnt(0x0F70 | (MYR + 1));
+    if (NST == 3 && s + 1 < n_mine) __builtin_amdgcn_s_waitcnt(0x0F70 | (MYR + SCN));
     else __builtin_amdgcn_s_waitcnt(0x0F70);
     __syncthreads();                        // ... everyone's share; all are done with slice s - 1
     if (s + NST - 1 < n_mine) {
@@ -206,7 +242,7 @@ __global__ __launch_bounds__(64 * WM * WN * KG, KG > 1 ? WM * WN * KG / 4 : 2) v
 #pragma unroll
       for (int b = 0; b < NS; ++b)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) acc[a][b][e] = gelu(acc[a][b][e]);
+        for (int e = 0; e < 4; ++e) acc[a][b][e] = gelu_q8(acc[a][b][e]);
   }
   if (KG == 1) __syncthreads();              // the ring is free
   const unsigned xs = lds0 + 2048 * wave;
@@ -220,15 +256,16 @@ __global__ __launch_bounds__(64 * WM * WN * KG, KG > 1 ? WM * WN * KG / 4 : 2) v
     unsigned big[MS];
 #pragma unroll
     for (int a = 0; a < MS; ++a) {
-      big[a] = 0;
+      float x[NS / 2][8];
 #pragma unroll
-      for (int b = 0; b < NS; ++b)
+      for (int u = 0; u < NS / 2; ++u)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          if (fw + 32 * (b >> 1) + 8 * q16 + 4 * (b & 1) >= N) acc[a][b][e] = 0.0f;   // padding columns are zero
-          big[a] = max(big[a], finite_bits(acc[a][b][e]));
-        }
-      big[a] = max_across(big[a]);
+        for (int e = 0; e < 8; ++e) x[u][e] = fw + 32 * u + 8 * q16 < N ? acc[a][2 * u + (e >> 2)][e & 3] : 0.0f;   // padding columns are zero
+      big[a] = max_across(block_max(x));
+#pragma unroll
+      for (int u = 0; u < NS / 2; ++u)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) acc[a][2 * u + (e >> 2)][e & 3] = x[u][e];
     }
     if constexpr (WPB > 1) {
       if (kg == 0 && q16 == 0) {
@@ -253,7 +290,7 @@ __global__ __launch_bounds__(64 * WM * WN * KG, KG > 1 ? WM * WN * KG / 4 : 2) v
       for (int u = 0; u < NS / 2; ++u) {
         float y[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) y[e] = q8_scaled(acc[a][2 * u + (e >> 2)][e & 3], inv);
+        for (int e = 0; e < 8; ++e) y[e] = acc[a][2 * u + (e >> 2)][e & 3] * inv;
         *(__attribute__((address_space(3))) u32x2 *)(size_t)(xs + SEG * l16 + 32 * u + 8 * q16) =
             u32x2{pack_e4m3(y[0], y[1], y[2], y[3]), pack_e4m3(y[4], y[5], y[6], y[7])};
       }

@@ -191,12 +191,12 @@ inline int tile_order(int bm, int bn, long long n_mt, long long n_nt) {
 inline int tile_tokens(int kernel) { return kernel == 113 ? 96 : kernel == 161 ? 160 : kernel == 193 ? 192 : kernel >= 128 ? 128 : 64; }
 inline int tile_features(int kernel) { return kernel < 96 ? 64 : 128; }
 
-inline void plan_stream(int ns, int M, int N, int slices, GemmPlan *best) {
+// tile_us: a full tile's time with every CU at work; few: what one of a single tile takes less where the others idle
+inline void plan_stream(int ns, int M, int N, int slices, double tile_us, double few, GemmPlan *best) {
   static const double part[5] = {0, 0.50, 0.66, 0.82, 1.0};
   const int bn = 32 * ns;
   if (N < bn || M < 64 || slices < 2) return;
   const long long n_nt = (N + bn - 1) / bn, all = (M + 255LL) / 256 * n_nt;
-  const double tile_us = ns == 8 ? 1.5 * slices + 6.0 : 1.7 * slices + 8.0;
   for (int less = 0; less < 3; ++less) {   // full tiles for this many rounds, the rest of the token rows as tail tiles
     const long long rounds = (all + GEMM_CUS - 1) / GEMM_CUS - less;
     if (rounds < 0) break;
@@ -205,11 +205,16 @@ inline void plan_stream(int ns, int M, int N, int slices, GemmPlan *best) {
       if (M < 64 * ms) break;
       const long long tail = (rows + 64 * ms - 1) / (64 * ms) * n_nt, room = rounds * GEMM_CUS - n_mt * n_nt;
       const double tail_rounds = tail > room ? (double)((tail - room + GEMM_CUS - 1) / GEMM_CUS) : 0.0;
-      const double us = 3.0 + (rounds + tail_rounds * part[ms]) * tile_us;
+      const double idle = std::max(0.0, 1.0 - (n_mt * n_nt + tail) / (double)GEMM_CUS);
+      const double us = 3.0 + (rounds + tail_rounds * part[ms]) * tile_us * (1.0 - few * idle);
       if (n_mt * n_nt + tail <= 0x7fffffffLL && us < best->us)
         *best = GemmPlan{ns, (int)n_mt, (int)n_nt, ms, (int)(n_mt * n_nt + tail), us, 0};
     }
   }
+}
+
+inline void plan_stream(int ns, int M, int N, int slices, GemmPlan *best) {
+  plan_stream(ns, M, N, slices, ns == 8 ? 1.5 * slices + 6.0 : 1.7 * slices + 8.0, 0.0, best);
 }
 
 // tiles of a problem

@@ -4,6 +4,7 @@
 #include <cmath>
 
 #include "gemm_q8.hpp"
+#include "gemm_q8_few.hpp"
 #include "gemm_q8_stream.hpp"
 #include "pab_internal.hpp"
 #include "q8_plan.hpp"
@@ -60,9 +61,18 @@ template <int ACT, bool OUT8>
 int launch_product(const pab::GemmPlan &g, const pab::GemmQ8Params &p, hipStream_t st) {
   const dim3 persistent((unsigned)std::min(g.n_units, pab::GEMM_CUS)), tiles((unsigned)((g.n_units + 7) / 8 * 8));
   switch (g.kernel) {
-    case 8: hipLaunchKernelGGL((pab::gemm_q8_stream_kernel<8, ACT, OUT8>), persistent, dim3(256), 0, st, p); break;
+    case 8: hipLaunchKernelGGL((pab::gemm_q8_stream_kernel<8, 4, ACT, OUT8>), persistent, dim3(512), 0, st, p); break;
     case 9:
-      if constexpr (!OUT8) hipLaunchKernelGGL((pab::gemm_q8_stream_kernel<9, ACT, false>), persistent, dim3(256), 0, st, p);
+      if constexpr (!OUT8) hipLaunchKernelGGL((pab::gemm_q8_stream_kernel<9, 3, ACT, false>), persistent, dim3(512), 0, st, p);
+      break;
+    case 16:
+      if constexpr (!OUT8) hipLaunchKernelGGL((pab::gemm_q8_few_kernel<1, ACT>), dim3((unsigned)g.n_units), dim3(512), 0, st, p);
+      break;
+    case 32:
+      if constexpr (!OUT8) hipLaunchKernelGGL((pab::gemm_q8_few_kernel<2, ACT>), dim3((unsigned)g.n_units), dim3(512), 0, st, p);
+      break;
+    case 48:
+      if constexpr (!OUT8) hipLaunchKernelGGL((pab::gemm_q8_few_kernel<4, ACT>), dim3((unsigned)g.n_units), dim3(512), 0, st, p);
       break;
     case 64:
       if constexpr (!OUT8) hipLaunchKernelGGL((pab::gemm_q8_tile_kernel<2, 2, 2, 2, 3, 1, ACT, false>), tiles, dim3(256), 0, st, p);
@@ -70,7 +80,12 @@ int launch_product(const pab::GemmPlan &g, const pab::GemmQ8Params &p, hipStream
     case 65:
       if constexpr (!OUT8) hipLaunchKernelGGL((pab::gemm_q8_tile_kernel<2, 2, 2, 2, 3, 3, ACT, false>), tiles, dim3(768), 0, st, p);
       break;
+    case 96: hipLaunchKernelGGL((pab::gemm_q8_tile_kernel<2, 4, 2, 2, 3, 1, ACT, OUT8>), tiles, dim3(512), 0, st, p); break;
+    case 97: hipLaunchKernelGGL((pab::gemm_q8_tile_kernel<2, 4, 2, 2, 3, 2, ACT, OUT8>), tiles, dim3(1024), 0, st, p); break;
+    case 113: hipLaunchKernelGGL((pab::gemm_q8_tile_kernel<2, 2, 3, 4, 2, 2, ACT, OUT8>), tiles, dim3(512), 0, st, p); break;
     case 128: hipLaunchKernelGGL((pab::gemm_q8_tile_kernel<2, 2, 4, 4, 2, 1, ACT, OUT8>), tiles, dim3(256), 0, st, p); break;
+    case 129: hipLaunchKernelGGL((pab::gemm_q8_tile_kernel<2, 2, 4, 4, 2, 2, ACT, OUT8>), tiles, dim3(512), 0, st, p); break;
+    case 161: hipLaunchKernelGGL((pab::gemm_q8_tile_kernel<2, 2, 5, 4, 2, 2, ACT, OUT8>), tiles, dim3(512), 0, st, p); break;
     default: return fail(PAB_EINVAL, "no product kernel %d", g.kernel);
   }
   return launched();

@@ -1,20 +1,47 @@
-// Which tiles a product of 8-bit rows takes.  A slice of 128 bytes costs what a slice of 64 bf16 columns does (gemm_q8.hpp), so the estimates are
-// those of the bf16 projections (launch_plan.hpp) over half as many slices.
+// Which tiles a product of 8-bit rows takes: estimates as for the bf16 projections (launch_plan.hpp, with its kernel numbers), with constants of
+// their own, in us, at so many slices of 128.  A few tiles are bound by the latency of their K loop, more than one per CU by L2 and by their
+// stores.  Both sides of the lines, measured in us:
+//   16, 32, 48: gemm_q8_few for up to 16, 32, 64 tokens, against 64 x 64 tiles with K groups: 1 x 6912 x 1152 3.9 / 5.1, 3 x 3256 x 4440 5.8 / 9.9,
+//   17 x 1152 x 1152 3.5 / 5.0, 64 x 1152 x 1152 5.1 / 5.1, but 64 x 1152 x 4608 13.3 / 10.5, 20 x 4608 x 4608 14.3 / 10.3
+//   64 x 64 tiles, three K groups / one: 1 x 6912 x 1152 4.9 / 5.4, 1260 x 576 x 2304 7.5 / 8.6, but 1260 x 576 x 576 4.7 / 4.5
+//   96 x 128, two K groups / 128 x 128: 1260 x 2304 x 576 7.2 / 7.6, 2600 x 1152 x 4608 21.9 / 28.2
+//   160 x 128, two K groups / 128 x 128 / large tiles: 4413 x 1152 x 4608 28.2 / 32.2 / 41.2, 4413 x 1152 x 1152 11.3 / 12.3 / 15.2
+//   128 x 128 / large: 1260 x 3456 x 1152 11.7 / 14.3, 8000 x 1152 x 1152 20.1 / 18.5, 4413 x 4608 x 1152 35.7 / 31.0
+//   64 x 128 / 128 x 128, 8-bit outputs with GELU: 1260 x 1152 x 576 6.1 / 8.6, 1260 x 3456 x 1152 17.2 / 13.6
 #pragma once
+#include <algorithm>
+
 #include "launch_plan.hpp"
 
 namespace pab {
 
-// kernel numbers as in GemmPlan; 32: 32 tokens x 128 features (quantised outputs of few tokens: their tiles are whole blocks of 128)
+// base: launch, first copies, K groups' sums; latency: a slice of a lone tile; l2, out: a slice and the stores where every CU has a tile
+inline void q8_tile(int kernel, double base, double latency, double l2, double out, int M, int N, int slices, GemmPlan *best) {
+  const int bm = tile_tokens(kernel), bn = tile_features(kernel);
+  const long long n_mt = ((long long)M + bm - 1) / bm, n_nt = (N + bn - 1) / bn, all = n_mt * n_nt;
+  if (((kernel & 1) && all > GEMM_CUS) || all > 0x7ffffff0LL) return;   // K groups: one workgroup per CU
+  const double load = all / (double)GEMM_CUS + 0.25, us = base + slices * std::max(latency, load * l2) + load * out;
+  if (us < best->us) *best = GemmPlan{kernel, (int)n_mt, (int)n_nt, 0, (int)all, us, tile_order(bm, bn, n_mt, n_nt)};
+}
+
 inline GemmPlan plan_q8(int M, int N, int nk, bool out8) {
   GemmPlan best{0, 0, 0, 0, 0, 1e30, 0};
-  if (!out8) {
-    plan_tile(64, 2.9, 0.26, 0.25, 0.55, M, N, nk, &best);
-    plan_tile(65, 2.95, 0.185, 0.17, 0.55, M, N, nk, &best);
+  if (!out8 && M <= 64) {   // few tokens: 16 features per workgroup, which reads them and every token at about 38 KB / us
+    const int units = (N + 15) / 16;
+    best = GemmPlan{M <= 16 ? 16 : M <= 32 ? 32 : 48, 1, units, 0, units, 2.9 + (units + GEMM_CUS - 1) / GEMM_CUS * (16 + M) * 128.0 * nk / 38000.0, 0};
   }
-  plan_tile(128, 3.5, 0.55, 0.52, 2.2, M, N, nk, &best);
-  if (!out8 || N % 128 == 0) plan_stream(8, M, N, nk, &best);   // tiles moved back to the edge start at whole blocks
-  if (!out8) plan_stream(9, M, N, nk, &best);
+  if (!out8) {   // 8-bit outputs: tiles are whole blocks of 128 features
+    q8_tile(64, 2.15, 0.32, 0.22, 0.5, M, N, nk, &best);
+    q8_tile(65, 2.75, 0.227, 0.21, 0.5, M, N, nk, &best);
+  }
+  q8_tile(96, 2.4, 0.40, 0.41, 1.0, M, N, nk, &best);
+  q8_tile(97, 2.75, 0.335, 0.33, 1.0, M, N, nk, &best);
+  q8_tile(113, 2.7, 0.49, 0.46, 1.6, M, N, nk, &best);
+  q8_tile(128, 2.6, 0.66, 0.52, 2.0, M, N, nk, &best);
+  q8_tile(129, 3.2, 0.52, 0.50, 2.0, M, N, nk, &best);
+  q8_tile(161, 3.6, 0.58, 0.56, 2.5, M, N, nk, &best);
+  if (!out8 || N % 128 == 0) plan_stream(8, M, N, nk, 1.57 * nk + 5.5, 0.4, &best);   // tiles moved back to the edge start at whole blocks
+  if (!out8) plan_stream(9, M, N, nk, 1.69 * nk + 8.0, 0.4, &best);
   return best;
 }
 

@@ -151,7 +151,8 @@ def product_tolerance(a, av, b, bv, extra=0.0):
 
 SHAPES = [(1, 8, 8), (1, 6912, 1152), (2, 136, 128), (15, 64, 136), (17, 72, 320), (63, 248, 1152), (64, 256, 512), (65, 128, 640), (130, 264, 384),
           (257, 576, 576), (300, 1152, 4608), (1260, 1728, 576), (497, 3456, 1152), (2100, 1152, 1152), (700, 4608, 256), (5000, 40, 72), (2560, 3456, 1152), (6249, 1152, 640), (4200, 2304, 320), (9001, 584, 256), (17000, 256, 384),
-          (8192, 1024, 512), (3000, 2504, 1024)]
+          (8192, 1024, 512), (3000, 2504, 1024), (1, 1152, 128), (3, 3256, 4440), (16, 24, 1152), (31, 1152, 1160), (33, 520, 2304), (64, 1160, 1152),
+          (9, 8, 13000), (26000, 1152, 264), (13000, 2048, 768), (1500, 1000, 2304), (4413, 1152, 1152)]
 
 
 def check_product(M, N, K, act, bias, seed, ld=(0, 0)):
