@@ -1,4 +1,4 @@
-"""Compile libpab.so (HIP, gfx950 only) in-tree with hipcc, and the CPython binding of its two hottest calls with g++.
+"""Compile libpab.so (HIP, gfx950 only) in-tree with hipcc, and the CPython binding of its hottest calls with g++.
 
 The library needs hipcc and nothing else.  The binding is for Python callers, who do without it where it cannot be built."""
 from __future__ import annotations

@@ -16,7 +16,7 @@ PAB_HIDDEN int fail(int code, const char *fmt, ...) __attribute__((format(printf
 
 inline bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
-// 8-bit rows of [rows, K] in one buffer, as pab_q8_layout places them: bytes (0: too large), and the matrix at `buffer`
+// 8-bit rows of [rows, K] in one buffer, as pab_quantized_layout places them: bytes (0: too large), and the matrix at `buffer`
 PAB_HIDDEN size_t q8_bytes(long long rows, long long K);
 PAB_HIDDEN pab_q8 q8_at(void *buffer, long long rows, long long K);
 // checked launch of the quantising pass

@@ -44,7 +44,7 @@ int check_q8(const char *name, const pab_q8 *y, long long K) {
 int check_rows(long long rows, int K, int dtype) {
   if (!float_type(dtype)) return fail(PAB_EINVAL, "dtype %d is not bf16(0)/f32(1)", dtype);
   if (rows < 1 || K < 8 || K % 8) return fail(PAB_EINVAL, "rows=%lld must be >= 1, K=%d a positive multiple of 8", rows, K);
-  if (rows > (1LL << 31) || rows * blocks_of(K) > (1LL << 28) - 16)
+  if (rows > (1LL << 31) || rows * blocks_of(K) > (1LL << 28))
     return fail(PAB_EINVAL, "%lld rows of %d are too many for one launch", rows, K);
   return PAB_OK;
 }
@@ -254,7 +254,7 @@ int pab_dequantize(long long rows, int K, int dtype, const pab_q8 *y, const void
   p.x = x; p.gate = gate; p.out = out;
   p.ld = y->ld; p.ld_scale = y->ld_scale; p.ldx = ldx; p.ldo = ldo; p.K = K;
   p.nc = pab::divisor((unsigned)(K / 8));
-  if (rows * (K / 8) > 0xffffff00LL) return fail(PAB_EINVAL, "%lld rows of %d are too many for one launch", rows, K);
+  if (rows * (K / 8) > 0x7fffffffLL) return fail(PAB_EINVAL, "%lld rows of %d are too many for one launch", rows, K);
   p.n_item = (unsigned)(rows * (K / 8));
   const dim3 grid((unsigned)((p.n_item + 255LL) / 256));
   const hipStream_t st = static_cast<hipStream_t>(hip_stream);

@@ -61,6 +61,13 @@ def test_quantize_and_dequantize_refuse(rows, K, dtype, x, ldx):
         assert status("pab_dequantize", rows, K, dtype, q8(), x, ldx, 0, OK, 1152, None) == pab.EINVAL
 
 
+def test_dequantize_refuses_more_than_its_index_holds():
+    """2^31 chunks of 8 columns: the launch splits a chunk's number into row and column by a high product that is exact below that."""
+    y = q8(ld=4096, ld_scale=32)
+    assert status("pab_dequantize", 1 << 22, 4096, 0, y, 0, 0, 0, OK, 4096, None) == pab.EINVAL
+    assert "too many" in pab.pab_last_error()
+
+
 def test_dequantize_refuses_gate():
     assert status("pab_dequantize", 4, 1152, 0, q8(), 0, 0, OK + 4, OK, 1152, None) == pab.EINVAL
 
