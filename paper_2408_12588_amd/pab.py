@@ -776,6 +776,8 @@ def mlp_weights_quantized(shift, scale, w1: Q8, b1, w2: Q8, b2) -> pab_mlp_weigh
             continue
         if t.dtype is not torch.bfloat16 or t.numel() != n:
             raise ValueError("%s must be [%d] of bf16" % (name, n))
+    if any(t is not None and t.get_device() != w1.data.get_device() for t in (shift, scale, b1, w2.data, b2)):
+        raise ValueError("the weights are on different devices")
     w = pab_mlp_weights_quantized(_ptr(shift), _ptr(scale), w1.struct, _ptr(b1), w2.struct, _ptr(b2))
     w._keep = (shift, scale, w1, b1, w2, b2)
     w._shape = (hidden, inner)

@@ -212,3 +212,30 @@ def test_python_checks_its_tensors():
               lambda: pab.pab_rope_factors((1, 1), (2, 2))):
         with pytest.raises(ValueError):
             f()
+
+
+def test_mlp_weights_are_on_one_device():
+    import torch
+
+    class Stub:
+        """What the check looks at of a device tensor."""
+        dtype = torch.bfloat16
+
+        def __init__(self, n, device):
+            self.n, self.device = n, device
+
+        def numel(self):
+            return self.n
+
+        def get_device(self):
+            return self.device
+
+    def rows(n, K, device):
+        return pab._q8_of(type("data", (), {"shape": (n, K), "get_device": lambda self: device})(), None, K)
+
+    devices = [0] * 6
+    for i in range(6):
+        d = list(devices)
+        d[i] = 1
+        with pytest.raises(ValueError, match="different devices"):
+            pab.mlp_weights_quantized(Stub(64, d[0]), Stub(64, d[1]), rows(128, 64, d[2]), Stub(128, d[3]), rows(64, 128, d[4]), Stub(64, d[5]))
