@@ -1009,10 +1009,8 @@ int pab_attention_quantized(pab_ctx *ctx, int block, int kind, int step, const v
     const hipStream_t st = static_cast<hipStream_t>(hip_stream);
     int rc = launch_checked(kind, c.dtype, c.T, c.S, c.L, c.heads, c.head_dim, q, k, v, scratch, st);
     if (rc == PAB_OK) rc = pab::quantize(tok, C, c.dtype, scratch, C, &rows, st);
-    if (rc != PAB_OK) {
-      ctx->computed_step[(size_t)block * 3 + kind] = -1;   // the slot may hold parts of it
-      return rc;
-    }
+    if (rc == PAB_EDEVICE) ctx->computed_step[(size_t)block * 3 + kind] = -1;   // the slot may hold parts of it
+    if (rc != PAB_OK) return rc;
   }
   commit_cell(ctx, block, kind, step, decision);
   *out = rows;
@@ -1038,10 +1036,8 @@ int pab_module_attention_quantized(pab_ctx *ctx, int block, int kind, int step, 
     unsigned char *y = static_cast<unsigned char *>(scratch) + module_plane_bytes(c.T, c.S, c.L, c.heads, c.head_dim);
     int rc = launch_module(kind, c.T, c.S, c.L, c.heads, c.head_dim, x, text, w, scratch, scratch_bytes, y, st);
     if (rc == PAB_OK) rc = pab::quantize(tok, C, PAB_BF16, y, C, &rows, st);
-    if (rc != PAB_OK) {
-      ctx->computed_step[(size_t)block * 3 + kind] = -1;
-      return rc;
-    }
+    if (rc == PAB_EDEVICE) ctx->computed_step[(size_t)block * 3 + kind] = -1;
+    if (rc != PAB_OK) return rc;
   }
   commit_cell(ctx, block, kind, step, decision);
   *out = rows;

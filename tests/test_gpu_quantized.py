@@ -398,6 +398,28 @@ def test_captured_calls_follow_their_inputs():
         x.copy_(normal(100 + seed, n, C).bfloat16().to(DEV))
         graph.replay()
         torch.cuda.synchronize()
+def test_refused_computed_step_keeps_the_slot():
+    """A computed step that fails its checks launches nothing: the steps that reuse what the slot holds still may."""
+    wl = W.Workload("qr", 1, 4, 30, 20, 4, 72, "bf16", 8, (2, 2, 2), 1, 7, seed=7)
+    cfg = pab.config_of(wl)
+    eight = pab.QuantizedContext(cfg, DEV)
+    scratch = pab.module_scratch(wl.T, wl.S, wl.L, wl.heads, wl.head_dim, DEV)
+    kind = W.SPATIAL
+    w = pab.module_weights(**{n: t.to(DEV) for n, t in W.make_module_weights(wl, 0, kind).items()})
+    x = W.make_module_input(wl, 0, kind, 0).to(DEV)
+    steps = [pab.pab_schedule(kind, s, cfg.range_lo, cfg.range_hi, cfg.interval[kind]) for s in range(wl.n_steps)]
+    first_reuse = steps.index(pab.REUSE)
+    later = next(s for s in range(first_reuse, wl.n_steps) if steps[s] == pab.COMPUTE)
+    for s in range(first_reuse):
+        eight.pab_module_attention_quantized(0, kind, s, x, None, w, scratch)
+    for bad in (scratch[:256], None):
+        with pytest.raises(pab.PabError):
+            eight.pab_module_attention_quantized(0, kind, later, x, None, w, bad)
+    before = eight.workspace.clone()
+    assert eight.pab_module_attention_quantized(0, kind, first_reuse, None, None, None, None)[0] == pab.REUSE
+    assert torch.equal(before, eight.workspace)
+
+
         replayed = out.clone(), m.clone()
         out.zero_(), m.zero_()
         chain()
