@@ -80,7 +80,9 @@ int launch_product(const pab::GemmPlan &g, const pab::GemmQ8Params &p, hipStream
     case 65:
       if constexpr (!OUT8) hipLaunchKernelGGL((pab::gemm_q8_tile_kernel<2, 2, 2, 2, 3, 3, ACT, false>), tiles, dim3(768), 0, st, p);
       break;
-    case 96: hipLaunchKernelGGL((pab::gemm_q8_tile_kernel<2, 4, 2, 2, 3, 1, ACT, OUT8>), tiles, dim3(512), 0, st, p); break;
+    case 96:
+      if constexpr (OUT8) hipLaunchKernelGGL((pab::gemm_q8_tile_kernel<2, 4, 2, 2, 3, 1, ACT, true>), tiles, dim3(512), 0, st, p);
+      break;
     case 97: hipLaunchKernelGGL((pab::gemm_q8_tile_kernel<2, 4, 2, 2, 3, 2, ACT, OUT8>), tiles, dim3(1024), 0, st, p); break;
     case 113: hipLaunchKernelGGL((pab::gemm_q8_tile_kernel<2, 2, 3, 4, 2, 2, ACT, OUT8>), tiles, dim3(512), 0, st, p); break;
     case 128: hipLaunchKernelGGL((pab::gemm_q8_tile_kernel<2, 2, 4, 4, 2, 1, ACT, OUT8>), tiles, dim3(256), 0, st, p); break;

@@ -30,11 +30,12 @@ inline GemmPlan plan_q8(int M, int N, int nk, bool out8) {
     const int units = (N + 15) / 16;
     best = GemmPlan{M <= 16 ? 16 : M <= 32 ? 32 : 48, 1, units, 0, units, 2.9 + (units + GEMM_CUS - 1) / GEMM_CUS * (16 + M) * 128.0 * nk / 38000.0, 0};
   }
-  if (!out8) {   // 8-bit outputs: tiles are whole blocks of 128 features
+  if (out8) {    // tiles are whole blocks of 128 features
+    q8_tile(96, 2.4, 0.40, 0.41, 1.0, M, N, nk, &best);
+  } else {
     q8_tile(64, 2.15, 0.32, 0.22, 0.5, M, N, nk, &best);
     q8_tile(65, 2.75, 0.227, 0.21, 0.5, M, N, nk, &best);
   }
-  q8_tile(96, 2.4, 0.40, 0.41, 1.0, M, N, nk, &best);
   q8_tile(97, 2.75, 0.335, 0.33, 1.0, M, N, nk, &best);
   q8_tile(113, 2.7, 0.49, 0.46, 1.6, M, N, nk, &best);
   q8_tile(128, 2.6, 0.66, 0.52, 2.0, M, N, nk, &best);

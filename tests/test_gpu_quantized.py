@@ -152,7 +152,10 @@ def product_tolerance(a, av, b, bv, extra=0.0):
 SHAPES = [(1, 8, 8), (1, 6912, 1152), (2, 136, 128), (15, 64, 136), (17, 72, 320), (63, 248, 1152), (64, 256, 512), (65, 128, 640), (130, 264, 384),
           (257, 576, 576), (300, 1152, 4608), (1260, 1728, 576), (497, 3456, 1152), (2100, 1152, 1152), (700, 4608, 256), (5000, 40, 72), (2560, 3456, 1152), (6249, 1152, 640), (4200, 2304, 320), (9001, 584, 256), (17000, 256, 384),
           (8192, 1024, 512), (3000, 2504, 1024), (1, 1152, 128), (3, 3256, 4440), (16, 24, 1152), (31, 1152, 1160), (33, 520, 2304), (64, 1160, 1152),
-          (9, 8, 13000), (26000, 1152, 264), (13000, 2048, 768), (1500, 1000, 2304), (4413, 1152, 1152)]
+          (9, 8, 13000), (26000, 1152, 264), (13000, 2048, 768), (1500, 1000, 2304), (4413, 1152, 1152),
+          (23579, 656, 200), (32391, 832, 256), (24900, 792, 136), (29764, 1032, 136), (25815, 1296, 256), (26644, 1056, 200), (26890, 288, 136),
+          (25618, 536, 1160), (2211, 7680, 200), (4755, 6272, 136), (25334, 896, 256), (23558, 72, 896), (27081, 72, 760), (791, 5304, 896),
+          (371, 8288, 1160)]
 
 
 def check_product(M, N, K, act, bias, seed, ld=(0, 0)):
@@ -286,6 +289,31 @@ def test_offsets_past_32_bits():
     assert np.all(np.abs(c[picks].cpu().double().numpy() - lin) <= BF * np.abs(lin) + 1.01 * tol)
 
 
+@pytest.mark.parametrize("M,N,K,out8", [(40, 520, 1160, False), (300, 576, 1152, False), (300, 576, 1152, True), (25618, 536, 1160, False),
+                                        (16689, 640, 256, True)])
+def test_linear_widest_pitches(M, N, K, out8):
+    """Rows 2^24 bytes apart, whose offsets inside a tile pass 2^31 (the buffer starts 2^31 and more bytes before them): the bits of dense rows."""
+    rows, first, pitch = 640, 160, 1 << 24
+    buf = torch.empty(first + rows, pitch, dtype=torch.uint8, device=DEV)
+
+    def spread(q, column):
+        nb = qo.blocks(K)
+        d = buf[first:first + q.rows, column:column + 128 * nb]
+        s = buf[first:first + q.rows, column + (1 << 22):column + (1 << 22) + (nb + 3) // 4 * 4]
+        d.copy_(q.data), s.copy_(q.scale)
+        return pab.Q8(d, s, K)
+
+    a, _ = make_q8(normal(51, M, K))
+    w, _ = make_q8(normal(52, N, K) / K ** 0.5)
+    run = lambda a, w: pab.pab_linear_quantized(a, w, out=pab.q8_empty(M, N, DEV) if out8 else None)   # noqa: E731
+    dense = run(a, w)
+    far = run(spread(a, 1 << 23) if M <= rows else a, spread(w, 0))
+    if out8:
+        assert torch.equal(dense.data, far.data) and torch.equal(dense.scale[:, :qo.blocks(N)], far.scale[:, :qo.blocks(N)])
+    else:
+        assert torch.equal(dense, far)
+
+
 # ---- the MLP ----
 def mlp_case(n, C, F, seed):
     x = (normal(seed, n, C) * 2 + 0.5).bfloat16()
@@ -370,6 +398,28 @@ def test_module_slots_are_quantised_outputs():
             assert got == dec and torch.equal(slot.data, want.data) and torch.equal(slot.scale[:, :3], want.scale[:, :3])
 
 
+def test_refused_computed_step_keeps_the_slot():
+    """A computed step that fails its checks launches nothing: the steps that reuse what the slot holds still may."""
+    wl = W.Workload("qr", 1, 4, 30, 20, 4, 72, "bf16", 8, (2, 2, 2), 1, 7, seed=7)
+    cfg = pab.config_of(wl)
+    eight = pab.QuantizedContext(cfg, DEV)
+    scratch = pab.module_scratch(wl.T, wl.S, wl.L, wl.heads, wl.head_dim, DEV)
+    kind = W.SPATIAL
+    w = pab.module_weights(**{n: t.to(DEV) for n, t in W.make_module_weights(wl, 0, kind).items()})
+    x = W.make_module_input(wl, 0, kind, 0).to(DEV)
+    steps = [pab.pab_schedule(kind, s, cfg.range_lo, cfg.range_hi, cfg.interval[kind]) for s in range(wl.n_steps)]
+    first_reuse = steps.index(pab.REUSE)
+    later = next(s for s in range(first_reuse, wl.n_steps) if steps[s] == pab.COMPUTE)
+    for s in range(first_reuse):
+        eight.pab_module_attention_quantized(0, kind, s, x, None, w, scratch)
+    for bad in (scratch[:256], None):
+        with pytest.raises(pab.PabError):
+            eight.pab_module_attention_quantized(0, kind, later, x, None, w, bad)
+    before = eight.workspace.clone()
+    assert eight.pab_module_attention_quantized(0, kind, first_reuse, None, None, None, None)[0] == pab.REUSE
+    assert torch.equal(before, eight.workspace)
+
+
 # ---- graphs ----
 def test_captured_calls_follow_their_inputs():
     """Quantise, product into rows, product, residual and the MLP in a graph: every replay gives what the eager calls give."""
@@ -398,28 +448,6 @@ def test_captured_calls_follow_their_inputs():
         x.copy_(normal(100 + seed, n, C).bfloat16().to(DEV))
         graph.replay()
         torch.cuda.synchronize()
-def test_refused_computed_step_keeps_the_slot():
-    """A computed step that fails its checks launches nothing: the steps that reuse what the slot holds still may."""
-    wl = W.Workload("qr", 1, 4, 30, 20, 4, 72, "bf16", 8, (2, 2, 2), 1, 7, seed=7)
-    cfg = pab.config_of(wl)
-    eight = pab.QuantizedContext(cfg, DEV)
-    scratch = pab.module_scratch(wl.T, wl.S, wl.L, wl.heads, wl.head_dim, DEV)
-    kind = W.SPATIAL
-    w = pab.module_weights(**{n: t.to(DEV) for n, t in W.make_module_weights(wl, 0, kind).items()})
-    x = W.make_module_input(wl, 0, kind, 0).to(DEV)
-    steps = [pab.pab_schedule(kind, s, cfg.range_lo, cfg.range_hi, cfg.interval[kind]) for s in range(wl.n_steps)]
-    first_reuse = steps.index(pab.REUSE)
-    later = next(s for s in range(first_reuse, wl.n_steps) if steps[s] == pab.COMPUTE)
-    for s in range(first_reuse):
-        eight.pab_module_attention_quantized(0, kind, s, x, None, w, scratch)
-    for bad in (scratch[:256], None):
-        with pytest.raises(pab.PabError):
-            eight.pab_module_attention_quantized(0, kind, later, x, None, w, bad)
-    before = eight.workspace.clone()
-    assert eight.pab_module_attention_quantized(0, kind, first_reuse, None, None, None, None)[0] == pab.REUSE
-    assert torch.equal(before, eight.workspace)
-
-
         replayed = out.clone(), m.clone()
         out.zero_(), m.zero_()
         chain()
