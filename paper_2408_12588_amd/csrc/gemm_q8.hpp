@@ -71,29 +71,6 @@ __device__ __forceinline__ unsigned max_across(unsigned x) {
   return max(b[0], b[1]);
 }
 
-// The largest finite magnitude among a lane's values, as bits, and infinities become NaN: maxima of three without a look at each value (they
-// pass over NaNs), and only where that comes out infinite somewhere in the wavefront value by value.
-template <int N>
-__device__ __forceinline__ unsigned block_max(float (&x)[N][8]) {
-  float m = 0.0f;
-#pragma unroll
-  for (int u = 0; u < N; ++u)
-#pragma unroll
-    for (int e = 0; e < 8; e += 2) m = fmaxf(fmaxf(m, fabsf(x[u][e])), fabsf(x[u][e + 1]));
-  unsigned big = __float_as_uint(m);
-  if (__any(big >= 0x7f800000u)) {
-    big = 0;
-#pragma unroll
-    for (int u = 0; u < N; ++u)
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        big = max(big, finite_bits(x[u][e]));
-        x[u][e] = q8_scaled(x[u][e], 1.0f);
-      }
-  }
-  return big;
-}
-
 // GELU in its tanh form, x / (1 + exp(-2 u)), u = sqrt(2 / pi) (x + 0.044715 x^3) (products written out: the same bits wherever it is inlined)
 __device__ __forceinline__ float gelu_q8(float x) {
 #pragma clang fp contract(off)

@@ -42,9 +42,27 @@ __device__ __forceinline__ unsigned pack_e4m3(float a, float b, float c, float d
   int r = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
   return (unsigned)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, r, true);
 }
-// x / scale, NaN for what is not finite
-__device__ __forceinline__ float q8_scaled(float x, float inverse) {
-  return (__float_as_uint(x) & 0x7f800000u) == 0x7f800000u ? __uint_as_float(0x7fc00000u) : x * inverse;
+// The largest finite magnitude among a lane's values, as bits, and infinities become NaN: maxima of three without a look at each value (they
+// pass over NaNs), and only where that comes out infinite somewhere in the wavefront value by value.
+template <int N>
+__device__ __forceinline__ unsigned block_max(float (&x)[N][8]) {
+  float m = 0.0f;
+#pragma unroll
+  for (int u = 0; u < N; ++u)
+#pragma unroll
+    for (int e = 0; e < 8; e += 2) m = fmaxf(fmaxf(m, fabsf(x[u][e])), fabsf(x[u][e + 1]));
+  unsigned big = __float_as_uint(m);
+  if (__any(big >= 0x7f800000u)) {
+    big = 0;
+#pragma unroll
+    for (int u = 0; u < N; ++u)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        big = max(big, finite_bits(x[u][e]));
+        if (!isfinite(x[u][e])) x[u][e] = __uint_as_float(0x7fc00000u);
+      }
+  }
+  return big;
 }
 
 // largest of 16 neighbouring lanes, in all of them, by register moves
