@@ -10,6 +10,18 @@
 // stage and publishes the other, and the copies of the slice after that go out two per step, so that they have half a slice to arrive.
 // There is no branch inside a slice: the compiler sinks products past one, and then holds their operands.  The copies of a tile of fewer than 256
 // tokens repeat its last rows, and those behind the last tile repeat that tile; nobody reads either.
+//
+// Between tiles: the first slice of a tile, written out by itself, starts the sums from the bias, which was copied a tile ahead; its barrier does not
+// wait for the stores of the tile before (memory operations of a wavefront end in order, so leaving as many of the last ones open as
+// there were stores is enough); and the stores of a step of the epilogue go out behind the arithmetic of the next.
+//
+// Measured, us: a slice of 256 x 256 x 128 takes 1.57, of 256 x 288 1.69, and a tile 5.5 and 8.0 more (GELU, 8-bit outputs: about 2 more).
+// With all operands in L2 a slice takes 1.37, without the copies 1.08, and the products alone, from registers, 0.9 to 1.0 (the clock
+// falls under them: random values 3.6 to 4.1 PF, zeros 4.9).  So the way from L2 into LDS bounds the loop, and what could be done about
+// its time was: two copies per step (all at once 2.12; in the second half 1.8; one or three per step slower), 128-byte rows, tile orders
+// that share operands within an XCD (groups of 2 to 16 token tiles: the same).  Four wavefronts of 128 x 128 with 512 registers run the loop as
+// fast and leave a tile more slowly; touching the slice after next for L2 gains 3 % at K = 1152 and loses 9 % at 4608.  Whole
+// products: 25440 x 3456 x 1152 114 (1.78 PF), 57600 x 1152 x 4608 276 (2.2 PF), 16384 x 4096 x 1152 into 8-bit rows 70 (2.2 PF), with GELU 87.
 #pragma once
 #include "gemm_q8.hpp"
 
@@ -24,7 +36,7 @@ __global__ __launch_bounds__(512, 2) void gemm_q8_stream_kernel(const GemmQ8Para
   constexpr bool ODD = NS % 2 != 0;
   constexpr int W0 = 128 * BM, W1 = W0 + 128 * 64 * NPAIR, SC = 128 * ROWS;   // byte offsets in a stage
   constexpr int SHIFT1 = ODD ? 16 : 0;           // features of wave column 1 before its pairs
-  constexpr int NDMA = 4 + NPAIR + (ODD ? 1 : 0);   // copy rounds of a wavefront per slice (the last: wavefronts 0-3)
+  constexpr int NDMA = 4 + NPAIR + (ODD ? 1 : 0);   // copy rounds of a wavefront per slice
   constexpr int AHEAD = RING - 1, JB = NS - AHEAD;  // operand distance, barrier step
   constexpr int PER = 2;                         // copy rounds per step
   static_assert(NPAIR % 2 == 0, "pairs are stored two at a time");
@@ -141,8 +153,6 @@ __global__ __launch_bounds__(512, 2) void gemm_q8_stream_kernel(const GemmQ8Para
       const unsigned st = lds0 + STAGE * s;
       tb = st + 2048 * MS * wm + op;
       wb = st + W0 + 4096 * wn + op;
-      tb4 = tb ^ 64;
-      wb4 = wb ^ 64;
       tb4 = tb ^ 64;
       wb4 = wb ^ 64;
       tsb = st + SC + 4 * (16 * MS * wm + l16) + (k & 3);
