@@ -27,6 +27,7 @@ struct GemmQ8Params {
   int n_mt, n_nt;                    // token / feature tiles
   int by_feature, n_inner;           // consecutive tiles share their features (1) or their tokens (0), n_inner of them
   int ms_tail, n_units;              // large tiles: see gemm_q8_stream.hpp
+  int past;                          // the output goes past the caches
 };
 
 enum { Q8_NONE = 0, Q8_GELU = 1 };
@@ -61,6 +62,13 @@ __device__ __forceinline__ void dma4_to_lds(const void *base, unsigned voff, uns
                :
                : "v"(voff), "s"(base), "{m0}"(lds_addr)
                : "memory");
+}
+
+// 16 bytes of the output, past the caches or not.  In asm: the compiler makes one store of two to the same address and drops the hint.  The two cycles
+// behind it are the instruction's, before its data registers may be written again.
+__device__ __forceinline__ void put16(void *to, u32x4 v, int past) {
+  if (past) asm volatile("global_store_dwordx4 %0, %1, off nt\n\ts_nop 1" ::"v"(to), "v"(v) : "memory");
+  else *reinterpret_cast<u32x4 *>(to) = v;
 }
 
 // Largest finite magnitude of a token over the four lanes (lane bits 4 and 5) that hold its features
@@ -278,8 +286,7 @@ __global__ __launch_bounds__(64 * WM * WN * KG, KG > 1 ? WM * WN * KG / 4 : 2) v
       for (int i = 0; i < (16 * CPR + 63) / 64; ++i) {
         const int row = 64 / CPR * i + lane / CPR, mr = mw + 16 * a + row;
         if (row < 16 && mr < M && (fw & ~127) < N)         // a block that has a column is written whole
-          *reinterpret_cast<u32x4 *>(p.C8 + mr * p.ld8 + fw + 16 * (lane % CPR)) =
-              *(const __attribute__((address_space(3))) u32x4 *)(size_t)(xs + SEG * row + 16 * (lane % CPR));
+          put16(p.C8 + mr * p.ld8 + fw + 16 * (lane % CPR), *(const __attribute__((address_space(3))) u32x4 *)(size_t)(xs + SEG * row + 16 * (lane % CPR)), p.past);
       }
       __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     }
@@ -305,7 +312,7 @@ __global__ __launch_bounds__(64 * WM * WN * KG, KG > 1 ? WM * WN * KG / 4 : 2) v
         for (int i = 0; i < 16 / RPI; ++i) {
           const int row = RPI * i + lane / CPR, m = mw + 16 * a + row;
           const bf16x8 r = lds_read8(xs + 2 * SEG * row + 16 * xpos(row, lane % CPR));
-          if (m < M && n < N) *reinterpret_cast<bf16x8 *>(p.C + m * p.ldc + n) = r;   // N is a multiple of 8
+          if (m < M && n < N) put16(p.C + m * p.ldc + n, __builtin_bit_cast(u32x4, r), p.past);   // N is a multiple of 8
         }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
       }

@@ -235,8 +235,8 @@ __global__ __launch_bounds__(512, 2) void gemm_q8_stream_kernel(const GemmQ8Para
       unsigned char *dst = p.C8 + (m0 + (lane >> 3)) * p.ld8 + f0 + 16 * (lane & 7);
       u32x4 r0, r1;
       auto store = [&]() __attribute__((always_inline)) {
-        *reinterpret_cast<u32x4 *>(dst) = r0;
-        *reinterpret_cast<u32x4 *>(dst + 8 * p.ld8) = r1;
+        put16(dst, r0, p.past);
+        put16(dst + 8 * p.ld8, r1, p.past);
         dst += 16 * p.ld8;
       };
 #pragma unroll
@@ -272,8 +272,8 @@ __global__ __launch_bounds__(512, 2) void gemm_q8_stream_kernel(const GemmQ8Para
       bf16_t *dst = p.C + f0 + shift + 8 * (lane & 7) + (m0 + (lane >> 3)) * p.ldc;
       u32x4 r0, r1;
       auto store = [&](int i) __attribute__((always_inline)) {   // of step i: sub-tile i % MS, features 64 (i / MS)
-        *reinterpret_cast<u32x4 *>(dst) = r0;
-        *reinterpret_cast<u32x4 *>(dst + 8 * p.ldc) = r1;
+        put16(dst, r0, p.past);
+        put16(dst + 8 * p.ldc, r1, p.past);
         dst += i % MS == MS - 1 ? 64 - (MS - 1) * 16 * p.ldc : 16 * p.ldc;
       };
 #pragma unroll
@@ -305,8 +305,8 @@ __global__ __launch_bounds__(512, 2) void gemm_q8_stream_kernel(const GemmQ8Para
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 #pragma unroll
         for (int a = 0; a < (MS + 1) / 2; ++a) {
-          const bf16x8 r = lds_read8(xs + 1024 * a + 16 * lane);
-          if (2 * a + 1 < MS || lane < 32) *reinterpret_cast<bf16x8 *>(to + 32 * a * p.ldc) = r;
+          const u32x4 r = *(lds_cptr_u)(size_t)(xs + 1024 * a + 16 * lane);
+          if (2 * a + 1 < MS || lane < 32) *reinterpret_cast<u32x4 *>(to + 32 * a * p.ldc) = r;   // 32 bytes: half of what memory takes at once
         }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
       }

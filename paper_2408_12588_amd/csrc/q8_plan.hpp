@@ -31,18 +31,18 @@ inline GemmPlan plan_q8(int M, int N, int nk, bool out8) {
     best = GemmPlan{M <= 16 ? 16 : M <= 32 ? 32 : 48, 1, units, 0, units, 2.9 + (units + GEMM_CUS - 1) / GEMM_CUS * (16 + M) * 128.0 * nk / 38000.0, 0};
   }
   if (out8) {    // tiles are whole blocks of 128 features
-    q8_tile(96, 2.4, 0.40, 0.41, 1.0, M, N, nk, &best);
+    q8_tile(96, 2.06, 0.51, 0.4, 0.85, M, N, nk, &best);
   } else {
-    q8_tile(64, 2.15, 0.32, 0.22, 0.5, M, N, nk, &best);
-    q8_tile(65, 2.75, 0.227, 0.21, 0.5, M, N, nk, &best);
+    q8_tile(64, 2.03, 0.376, 0.3, 0.56, M, N, nk, &best);
+    q8_tile(65, 3.1, 0.157, 0.177, 0.65, M, N, nk, &best);
   }
-  q8_tile(97, 2.75, 0.335, 0.33, 1.0, M, N, nk, &best);
-  q8_tile(113, 2.7, 0.49, 0.46, 1.6, M, N, nk, &best);
-  q8_tile(128, 2.6, 0.66, 0.52, 2.0, M, N, nk, &best);
-  q8_tile(129, 3.2, 0.52, 0.50, 2.0, M, N, nk, &best);
-  q8_tile(161, 3.6, 0.58, 0.56, 2.5, M, N, nk, &best);
-  if (!out8 || N % 128 == 0) plan_stream(8, M, N, nk, 1.57 * nk + 5.5, 0.4, &best);   // tiles moved back to the edge start at whole blocks
-  if (!out8) plan_stream(9, M, N, nk, 1.69 * nk + 8.0, 0.4, &best);
+  q8_tile(97, 3.1, 0.28, 0.3, 0.87, M, N, nk, &best);
+  q8_tile(113, 2.5, 0.51, 0.436, 1.4, M, N, nk, &best);
+  q8_tile(128, 2.13, 0.88, 0.514, 1.6, M, N, nk, &best);
+  q8_tile(129, 2.93, 0.66, 0.51, 2.24, M, N, nk, &best);
+  q8_tile(161, 3.1, 0.7, 0.586, 2.35, M, N, nk, &best);
+  if (!out8 || N % 128 == 0) plan_stream(8, M, N, nk, 1.58 * nk + 4.7, 0.46, &best);   // tiles moved back to the edge start at whole blocks
+  if (!out8) plan_stream(9, M, N, nk, 1.70 * nk + 8.0, 0.34, &best);
   return best;
 }
 

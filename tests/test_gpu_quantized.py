@@ -155,7 +155,9 @@ SHAPES = [(1, 8, 8), (1, 6912, 1152), (2, 136, 128), (15, 64, 136), (17, 72, 320
           (9, 8, 13000), (26000, 1152, 264), (13000, 2048, 768), (1500, 1000, 2304), (4413, 1152, 1152),
           (23579, 656, 200), (32391, 832, 256), (24900, 792, 136), (29764, 1032, 136), (25815, 1296, 256), (26644, 1056, 200), (26890, 288, 136),
           (25618, 536, 1160), (2211, 7680, 200), (4755, 6272, 136), (25334, 896, 256), (23558, 72, 896), (27081, 72, 760), (791, 5304, 896),
-          (371, 8288, 1160)]
+          (371, 8288, 1160), (485, 5448, 896), (3138, 1160, 1000), (6705, 520, 1000), (275, 9136, 512),
+          (25113, 648, 200), (32606, 776, 136), (36518, 520, 256), (29714, 1040, 680), (21395, 1544, 760), (37269, 784, 136), (31964, 288, 200), (3969, 4736, 200),
+          (32244, 896, 136), (16519, 1408, 256)]
 
 
 def check_product(M, N, K, act, bias, seed, ld=(0, 0)):
@@ -287,6 +289,33 @@ def test_offsets_past_32_bits():
     lin = want @ wv.T
     tol = product_tolerance(sub, want, w, wv)
     assert np.all(np.abs(c[picks].cpu().double().numpy() - lin) <= BF * np.abs(lin) + 1.01 * tol)
+
+
+LARGE = [(24000, 3520, 384, False), (80000, 1152, 768, False), (45000, 3712, 264, True)]
+
+
+@pytest.mark.parametrize("M,N,K,out8", LARGE)
+def test_linear_large_outputs(M, N, K, out8):
+    """Outputs that large tiles write past the caches: the bits of rows that start between multiples of 64 bytes, which are written through
+    them, and some rows against the definition."""
+    a, av = make_q8(normal(61, M, K))
+    w, wv = make_q8(normal(62, N, K) / K ** 0.5)
+    rows = np.unique(np.concatenate([np.arange(0, M, 997), np.arange(M - 70, M), np.arange(250, 260)]))
+    sub = pab.Q8(a.data[rows], a.scale[rows], K)
+    want, tol = av[rows] @ wv.T, product_tolerance(sub, av[rows], w, wv)
+    if out8:
+        far = pab.pab_linear_quantized(a, w, out=pab.q8_empty(M, N, DEV))
+        d, s = torch.zeros(M, N + 16, dtype=torch.uint8, device=DEV), torch.zeros(M, 32, dtype=torch.uint8, device=DEV)
+        near = pab.pab_linear_quantized(a, w, out=pab.Q8(d, s, N))
+        nb = qo.blocks(N)
+        assert torch.equal(far.data, near.data[:, :N]) and torch.equal(far.scale[:, :nb], near.scale[:, :nb]) and not bool(d[:, N:].any())
+        check_rows_near(pab.Q8(far.data[rows], far.scale[rows], N), want, tol, N)
+    else:
+        far = pab.pab_linear_quantized(a, w)
+        buf = torch.zeros(M, N + 8, dtype=torch.bfloat16, device=DEV)
+        near = pab.pab_linear_quantized(a, w, out=buf[:, :N])
+        assert torch.equal(far, near) and not bool(buf[:, N:].any())
+        assert np.all(np.abs(far[rows].cpu().double().numpy() - want) <= BF * np.abs(want) + tol * (1 + BF))
 
 
 @pytest.mark.parametrize("M,N,K,out8", [(40, 520, 1160, False), (300, 576, 1152, False), (300, 576, 1152, True), (25618, 536, 1160, False),

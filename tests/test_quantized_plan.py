@@ -77,6 +77,12 @@ def test_every_planned_kernel_is_launched_and_covers_the_matrix(plan, out8, kern
             assert not kernel & 1 or units <= 256
 
 
+def test_large_outputs_are_large_enough(plan):
+    """... to be written past the caches, by large tiles of either width."""
+    assert all(M * N * (1 if out8 else 2) > 150 << 20 for M, N, K, out8 in G.LARGE)
+    assert [plan([s[:3]], int(s[3]))[0][0] for s in G.LARGE] == [8, 9, 8]
+
+
 def test_few_tokens_take_their_kernel_where_it_is_faster(plan):
     """Both sides of the line as measured."""
     assert [g[0] for g in plan([(1, 6912, 1152), (3, 3256, 4440), (17, 1152, 1152)], 0)] == [16, 16, 32]
