@@ -13,15 +13,17 @@
 //
 // Between tiles: the first slice of a tile, written out by itself, starts the sums from the bias, which was copied a tile ahead; its barrier does not
 // wait for the stores of the tile before (memory operations of a wavefront end in order, so leaving as many of the last ones open as
-// there were stores is enough); and the stores of a step of the epilogue go out behind the arithmetic of the next.
+// there were stores is enough); and the stores of a step of the epilogue go out behind the arithmetic of the next.  Large outputs are written past
+// the caches (q8_api.hip says when): what all workgroups of an XCD store at once is as large as its L2, and drives out the operands.  The 32-byte
+// pieces of odd sub-tiles never are: memory would read what it keeps of them (288-feature tiles, 53536 x 3584 x 200: 92 -> 135).
 //
-// Measured, us: a slice of 256 x 256 x 128 takes 1.57, of 256 x 288 1.69, and a tile 5.5 and 8.0 more (GELU, 8-bit outputs: about 2 more).
+// Measured, us: a slice of 256 x 256 x 128 takes 1.58, of 256 x 288 1.70, and a tile 3 (8-bit or large outputs) to 5 and 8 more, with GELU 3 more.
 // With all operands in L2 a slice takes 1.37, without the copies 1.08, and the products alone, from registers, 0.9 to 1.0 (the clock
 // falls under them: random values 3.6 to 4.1 PF, zeros 4.9).  So the way from L2 into LDS bounds the loop, and what could be done about
 // its time was: two copies per step (all at once 2.12; in the second half 1.8; one or three per step slower), 128-byte rows, tile orders
 // that share operands within an XCD (groups of 2 to 16 token tiles: the same).  Four wavefronts of 128 x 128 with 512 registers run the loop as
 // fast and leave a tile more slowly; touching the slice after next for L2 gains 3 % at K = 1152 and loses 9 % at 4608.  Whole
-// products: 25440 x 3456 x 1152 114 (1.78 PF), 57600 x 1152 x 4608 276 (2.2 PF), 16384 x 4096 x 1152 into 8-bit rows 70 (2.2 PF), with GELU 87.
+// products: 25440 x 3456 x 1152 98 (2.07 PF), 57600 x 1152 x 4608 273 (2.24 PF), 16384 x 4096 x 1152 into 8-bit rows 70 (2.2 PF), with GELU 83.
 #pragma once
 #include "gemm_q8.hpp"
 
