@@ -127,7 +127,7 @@ int product(int M, int N, int K, const pab_q8 *A, const pab_q8 *W, const void *b
     p.ld8 = C8->ld; p.ls8 = C8->ld_scale;
   }
   p.M = M; p.N = N; p.nk = (int)blocks_of(K);
-  const pab::GemmPlan g = pab::plan_q8(M, N, p.nk, C8 != nullptr);
+  const pab::GemmPlan g = pab::plan_q8(M, N, p.nk, C8 != nullptr, act == PAB_GELU);
   if (!g.kernel || g.n_units > 0xfffff0) return fail(PAB_EINVAL, "M=%d N=%d: matrix too large for one launch", M, N);
   p.n_mt = g.n_mt; p.n_nt = g.n_nt; p.by_feature = g.by_feature; p.n_inner = g.by_feature ? g.n_mt : g.n_nt;
   p.ms_tail = g.ms_tail; p.n_units = g.n_units;

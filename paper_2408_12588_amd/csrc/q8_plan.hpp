@@ -17,32 +17,35 @@
 
 namespace pab {
 
+// GELU with K groups, one of which applies it to all sums: 501 x 2816 x 640 into rows, 64 x 128 tiles, two groups / one 6.9 / 6.4
+constexpr double GELU_US = 0.8;
+
 // base: launch, first copies, K groups' sums; latency: a slice of a lone tile; l2, out: a slice and the stores where every CU has a tile
-inline void q8_tile(int kernel, double base, double latency, double l2, double out, int M, int N, int slices, GemmPlan *best) {
+inline void q8_tile(int kernel, bool gelu, double base, double latency, double l2, double out, int M, int N, int slices, GemmPlan *best) {
   const int bm = tile_tokens(kernel), bn = tile_features(kernel);
   const long long n_mt = ((long long)M + bm - 1) / bm, n_nt = (N + bn - 1) / bn, all = n_mt * n_nt;
   if (((kernel & 1) && all > GEMM_CUS) || all > 0x7ffffff0LL) return;   // K groups: one workgroup per CU
-  const double load = all / (double)GEMM_CUS + 0.25, us = base + slices * std::max(latency, load * l2) + load * out;
+  const double load = all / (double)GEMM_CUS + 0.25, us = base + (gelu && (kernel & 1) ? GELU_US : 0.0) + slices * std::max(latency, load * l2) + load * out;
   if (us < best->us) *best = GemmPlan{kernel, (int)n_mt, (int)n_nt, 0, (int)all, us, tile_order(bm, bn, n_mt, n_nt)};
 }
 
-inline GemmPlan plan_q8(int M, int N, int nk, bool out8) {
+inline GemmPlan plan_q8(int M, int N, int nk, bool out8, bool gelu) {
   GemmPlan best{0, 0, 0, 0, 0, 1e30, 0};
   if (!out8 && M <= 64) {   // few tokens: 16 features per workgroup, which reads them and every token at about 38 KB / us
     const int units = (N + 15) / 16;
     best = GemmPlan{M <= 16 ? 16 : M <= 32 ? 32 : 48, 1, units, 0, units, 2.9 + (units + GEMM_CUS - 1) / GEMM_CUS * (16 + M) * 128.0 * nk / 38000.0, 0};
   }
   if (out8) {    // tiles are whole blocks of 128 features
-    q8_tile(96, 2.06, 0.51, 0.4, 0.85, M, N, nk, &best);
+    q8_tile(96, gelu, 2.06, 0.51, 0.4, 0.85, M, N, nk, &best);
   } else {
-    q8_tile(64, 2.03, 0.376, 0.3, 0.56, M, N, nk, &best);
-    q8_tile(65, 3.1, 0.157, 0.177, 0.65, M, N, nk, &best);
+    q8_tile(64, gelu, 2.03, 0.376, 0.3, 0.56, M, N, nk, &best);
+    q8_tile(65, gelu, 3.1, 0.157, 0.177, 0.65, M, N, nk, &best);
   }
-  q8_tile(97, 3.1, 0.28, 0.3, 0.87, M, N, nk, &best);
-  q8_tile(113, 2.5, 0.51, 0.436, 1.4, M, N, nk, &best);
-  q8_tile(128, 2.13, 0.88, 0.514, 1.6, M, N, nk, &best);
-  q8_tile(129, 2.93, 0.66, 0.51, 2.24, M, N, nk, &best);
-  q8_tile(161, 3.1, 0.7, 0.586, 2.35, M, N, nk, &best);
+  q8_tile(97, gelu, 3.1, 0.28, 0.3, 0.87, M, N, nk, &best);
+  q8_tile(113, gelu, 2.5, 0.51, 0.436, 1.4, M, N, nk, &best);
+  q8_tile(128, gelu, 2.13, 0.88, 0.514, 1.6, M, N, nk, &best);
+  q8_tile(129, gelu, 2.93, 0.66, 0.51, 2.24, M, N, nk, &best);
+  q8_tile(161, gelu, 3.1, 0.7, 0.586, 2.35, M, N, nk, &best);
   if (!out8 || N % 128 == 0) plan_stream(8, M, N, nk, 1.58 * nk + 4.7, 0.46, &best);   // tiles moved back to the edge start at whole blocks
   if (!out8) plan_stream(9, M, N, nk, 1.70 * nk + 8.0, 0.34, &best);
   return best;

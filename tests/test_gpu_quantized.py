@@ -156,7 +156,8 @@ SHAPES = [(1, 8, 8), (1, 6912, 1152), (2, 136, 128), (15, 64, 136), (17, 72, 320
           (23579, 656, 200), (32391, 832, 256), (24900, 792, 136), (29764, 1032, 136), (25815, 1296, 256), (26644, 1056, 200), (26890, 288, 136),
           (25618, 536, 1160), (2211, 7680, 200), (4755, 6272, 136), (25334, 896, 256), (23558, 72, 896), (27081, 72, 760), (791, 5304, 896),
           (371, 8288, 1160), (485, 5448, 896), (3138, 1160, 1000), (6705, 520, 1000), (275, 9136, 512),
-          (25113, 648, 200), (32606, 776, 136), (36518, 520, 256), (29714, 1040, 680), (21395, 1544, 760), (37269, 784, 136), (31964, 288, 200), (3969, 4736, 200),
+          (25113, 648, 200), (32606, 776, 136), (36518, 520, 256), (29714, 1040, 680), (21395, 1544, 760), (37269, 784, 136), (31964, 288, 200),
+          (4959, 536, 1400), (774, 4800, 1536), (592, 6456, 1400), (6600, 536, 1600), (260, 9120, 1104), (3969, 4736, 200),
           (32244, 896, 136), (16519, 1408, 256)]
 
 

@@ -74,7 +74,7 @@ def test_dequantize_refuses_gate():
 
 @pytest.mark.parametrize("M,N,K,bias,act,C,ldc,out8", [
     (0, 1152, 1152, 0, 0, OK, 1152, None), (4, 0, 1152, 0, 0, OK, 1152, None), (4, 1148, 1152, 0, 0, OK, 1152, None),
-    (4, 1152, 1148, 0, 0, OK, 1152, None), (4, 1152, 0, 0, 0, OK, 1152, None), (4, 1152, 1152, OK + 8, 0, OK, 1152, None),
+    (4, 1152, 1148, 0, 0, OK, 1152, None), (260, 9120, 1100, 0, 0, OK, 9120, None), (4, 1152, 0, 0, 0, OK, 1152, None), (4, 1152, 1152, OK + 8, 0, OK, 1152, None),
     (4, 1152, 1152, 0, 2, OK, 1152, None), (4, 1152, 1152, 0, -1, OK, 1152, None), (4, 1152, 1152, 0, 0, 0, 1152, None),
     (4, 1152, 1152, 0, 0, OK, 1152, q8()), (4, 1152, 1152, 0, 0, OK + 8, 1152, None), (4, 1152, 1152, 0, 0, OK, 1144, None),
     (4, 1152, 1152, 0, 0, OK, 1156, None), (2**31 - 1, 1152, 1152, 0, 0, OK, 1152, None)])

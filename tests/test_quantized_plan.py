@@ -14,9 +14,9 @@ QUERY = r'''
 #include <cstdio>
 #include "q8_plan.hpp"
 int main() {
-  int M, N, nk, out8;
-  while (scanf("%d %d %d %d", &M, &N, &nk, &out8) == 4) {
-    const pab::GemmPlan g = pab::plan_q8(M, N, nk, out8);
+  int M, N, nk, out8, gelu;
+  while (scanf("%d %d %d %d %d", &M, &N, &nk, &out8, &gelu) == 5) {
+    const pab::GemmPlan g = pab::plan_q8(M, N, nk, out8, gelu);
     printf("%d %d %d %d %d\n", g.kernel, g.n_mt, g.n_nt, g.ms_tail, g.n_units);
   }
 }
@@ -32,8 +32,8 @@ def plan(tmp_path_factory):
     exe = str(d / "query")
     subprocess.run(["g++", "-std=c++17", "-O1", "-Wall", "-I", CSRC, "-o", exe, str(d / "query.cpp")], check=True, timeout=120)
 
-    def ask(shapes, out8):
-        text = "".join("%d %d %d %d\n" % (M, N, -(-K // 128), out8) for M, N, K in shapes)
+    def ask(shapes, out8, gelu=0):
+        text = "".join("%d %d %d %d %d\n" % (M, N, -(-K // 128), out8, gelu) for M, N, K in shapes)
         out = subprocess.run([exe], input=text, capture_output=True, text=True, check=True, timeout=60).stdout
         got = [tuple(int(x) for x in line.split()) for line in out.splitlines()]
         assert len(got) == len(shapes)
@@ -43,8 +43,9 @@ def plan(tmp_path_factory):
 
 
 def test_tested_shapes_reach_every_kernel(plan):
-    assert {g[0] for g in plan(G.SHAPES, 0)} == TO_VALUES
-    assert {g[0] for g in plan(G.SHAPES, 1)} == TO_ROWS
+    for gelu in (0, 1):
+        assert {g[0] for g in plan(G.SHAPES, 0, gelu)} == TO_VALUES
+        assert {g[0] for g in plan(G.SHAPES, 1, gelu)} == TO_ROWS
     # large tiles: every height of a tail, alone and behind full tiles, and workgroups that go through both
     large = {(out8, g[0], g[3], g[1] > 0, g[4] > 256) for out8 in (0, 1) for g in plan(G.SHAPES, out8) if g[0] in (8, 9) and g[1] * g[2] < g[4]}
     assert {(o, k, ms, True, True) for o, k in ((0, 8), (0, 9), (1, 8)) for ms in (1, 2, 3)} <= large, large
