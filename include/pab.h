@@ -426,7 +426,8 @@ int pab_dequantize(long long rows, int K, int dtype, const pab_q8 *y, const void
  * bf16 C [M, N] with a row pitch of ldc elements, rounded once, or 8-bit rows
  * C8 [M, N] (quantised from the fp32 sums); exactly one of the two is given.  C and C8 must not overlap A or W.  One launch on `hip_stream`.
  * PAB_EINVAL: M < 1, N or K not a positive multiple of 8, unknown act, both or
- * neither output, NULL or misaligned pointers, bad pitches.
+ * neither output, NULL or misaligned pointers, bad pitches, M or N above
+ * 2^31 - 1024 or more tiles than one launch holds (matrices of several 100 GB).
  * Sums below the smallest normal fp32 number may be lost.
  */
 enum pab_activation { PAB_NONE = 0, PAB_GELU = 1 };

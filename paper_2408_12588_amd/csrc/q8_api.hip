@@ -128,7 +128,7 @@ int product(int M, int N, int K, const pab_q8 *A, const pab_q8 *W, const void *b
   }
   p.M = M; p.N = N; p.nk = (int)blocks_of(K);
   const pab::GemmPlan g = pab::plan_q8(M, N, p.nk, C8 != nullptr, act == PAB_GELU);
-  if (!g.kernel || g.n_units > 0xfffff0) return fail(PAB_EINVAL, "M=%d N=%d: matrix too large for one launch", M, N);
+  if (!g.kernel) return fail(PAB_EINVAL, "M=%d N=%d: matrix too large for one launch", M, N);
   p.n_mt = g.n_mt; p.n_nt = g.n_nt; p.by_feature = g.by_feature; p.n_inner = g.by_feature ? g.n_mt : g.n_nt;
   p.ms_tail = g.ms_tail; p.n_units = g.n_units;
   p.past = C8 ? past_caches(g, M, C8->data, 128 * blocks_of(N), C8->ld) : past_caches(g, M, C, 2LL * N, 2 * ldc);

@@ -20,18 +20,28 @@ namespace pab {
 // GELU with K groups, one of which applies it to all sums: 501 x 2816 x 640 into rows, 64 x 128 tiles, two groups / one 6.9 / 6.4
 constexpr double GELU_US = 0.8;
 
+// Sizes that a launch and the kernels' 32-bit indexes hold.  A grid has fewer than 2^32 threads: 12.5 million workgroups of 512 (1 token, 200 million features
+// in kernel 16) are too many, where a quarter of them of 256 (kernel 64) are not.  The last tile's indexes end less than 512 past the matrix.
+constexpr int Q8_MOST = 0x7fffffff - 511;
+inline int q8_threads(int kernel) {
+  return kernel == 97 ? 1024 : kernel == 65 ? 768 : kernel == 64 || kernel == 128 ? 256 : 512;
+}
+inline bool q8_fits(int kernel, long long units) { return (units + 7) / 8 * 8 * q8_threads(kernel) < 1LL << 32; }   // grids are multiples of 8
+
 // base: launch, first copies, K groups' sums; latency: a slice of a lone tile; l2, out: a slice and the stores where every CU has a tile
 inline void q8_tile(int kernel, bool gelu, double base, double latency, double l2, double out, int M, int N, int slices, GemmPlan *best) {
   const int bm = tile_tokens(kernel), bn = tile_features(kernel);
-  const long long n_mt = ((long long)M + bm - 1) / bm, n_nt = (N + bn - 1) / bn, all = n_mt * n_nt;
-  if (((kernel & 1) && all > GEMM_CUS) || all > 0x7ffffff0LL) return;   // K groups: one workgroup per CU
+  const long long n_mt = ((long long)M + bm - 1) / bm, n_nt = ((long long)N + bn - 1) / bn, all = n_mt * n_nt;
+  if (((kernel & 1) && all > GEMM_CUS) || !q8_fits(kernel, all)) return;   // K groups: one workgroup per CU
   const double load = all / (double)GEMM_CUS + 0.25, us = base + (gelu && (kernel & 1) ? GELU_US : 0.0) + slices * std::max(latency, load * l2) + load * out;
   if (us < best->us) *best = GemmPlan{kernel, (int)n_mt, (int)n_nt, 0, (int)all, us, tile_order(bm, bn, n_mt, n_nt)};
 }
 
+// kernel 0: no launch holds the problem
 inline GemmPlan plan_q8(int M, int N, int nk, bool out8, bool gelu) {
   GemmPlan best{0, 0, 0, 0, 0, 1e30, 0};
-  if (!out8 && M <= 64) {   // few tokens: 16 features per workgroup, which reads them and every token at about 38 KB / us
+  if (M > Q8_MOST || N > Q8_MOST) return best;
+  if (!out8 && M <= 64 && q8_fits(16, (N + 15) / 16)) {   // few tokens: 16 features per workgroup, which reads them and every token at about 38 KB / us
     const int units = (N + 15) / 16;
     best = GemmPlan{M <= 16 ? 16 : M <= 32 ? 32 : 48, 1, units, 0, units, 2.9 + (units + GEMM_CUS - 1) / GEMM_CUS * (16 + M) * 128.0 * nk / 38000.0, 0};
   }
@@ -48,6 +58,7 @@ inline GemmPlan plan_q8(int M, int N, int nk, bool out8, bool gelu) {
   q8_tile(161, gelu, 3.1, 0.7, 0.586, 2.35, M, N, nk, &best);
   if (!out8 || N % 128 == 0) plan_stream(8, M, N, nk, 1.58 * nk + 4.7, 0.46, &best);   // tiles moved back to the edge start at whole blocks
   if (!out8) plan_stream(9, M, N, nk, 1.70 * nk + 8.0, 0.34, &best);
+  if (best.n_units > Q8_MOST) best.kernel = 0;
   return best;
 }
 

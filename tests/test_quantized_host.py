@@ -82,6 +82,13 @@ def test_linear_refuses(M, N, K, bias, act, C, ldc, out8):
     assert status("pab_linear_quantized", M, N, K, q8(), q8(), bias, act, C, ldc, out8, None) == pab.EINVAL
 
 
+@pytest.mark.parametrize("M,N", [(1, 2**31 - 8), (64, 2**31 - 256), (2**31 - 1, 8)])
+def test_linear_refuses_what_its_indexes_do_not_hold(M, N):
+    y = q8(ld=128, ld_scale=4)
+    assert status("pab_linear_quantized", M, N, 8, y, y, 0, 0, OK, N, None, None) == pab.EINVAL
+    assert "too large" in pab.pab_last_error()
+
+
 def test_linear_refuses_null_operands():
     assert status("pab_linear_quantized", 4, 1152, 1152, None, q8(), 0, 0, OK, 1152, None, None) == pab.EINVAL
     assert status("pab_linear_quantized", 4, 1152, 1152, q8(), None, 0, 0, OK, 1152, None, None) == pab.EINVAL

@@ -88,3 +88,26 @@ def test_few_tokens_take_their_kernel_where_it_is_faster(plan):
     """Both sides of the line as measured."""
     assert [g[0] for g in plan([(1, 6912, 1152), (3, 3256, 4440), (17, 1152, 1152)], 0)] == [16, 16, 32]
     assert not {g[0] for g in plan([(64, 1152, 4608), (20, 4608, 4608)], 0)} & {16, 32, 48}
+
+
+def test_launches_have_fewer_threads_than_a_grid_holds(plan):
+    """2^32 threads, workgroups of each kernel's own size counted in whole eights; matrices whose indexes would pass 2^31 have no kernel."""
+    body = open(os.path.join(CSRC, "q8_api.hip")).read()
+    body = body[body.index("int launch_product("):]
+    threads = {int(k): int(t) for k, t in re.findall(r"case (\d+):[^;]*?dim3\((\d+)\), 0, st, p\)", body[:body.index("\n}\n")])}
+    assert set(threads) == TO_VALUES | TO_ROWS
+    sizes = [2**30, 2**28 * 3 + 8, 2**31 - 1024, 2**31 - 520, 200_000_000, 100_000_000, 16777216, 1_000_008]
+    shapes = [(M, N, 8) for N in sizes for M in (1, 17, 64, 65, 4000)] + [(M, N, K) for M in sizes for N in (8, 136, 1152, 40000) for K in (8, 4608)]
+    for out8 in (0, 1):
+        got = plan(shapes, out8)
+        for (M, N, K), (kernel, n_mt, n_nt, ms, units) in zip(shapes, got):
+            if not kernel:
+                taken = 128 * -(-K // 128) * (M + N) + M * (128 * -(-N // 128) if out8 else 2 * N)
+                assert taken > 288 * 2**30 or max(M, N) > 2**31 - 1024, (M, N, K)   # only what the memory does not hold either
+                continue
+            assert units > 0, (M, N, K)
+            groups = min(units, 256) if kernel < 16 else (units + 7) // 8 * 8
+            assert groups * threads[kernel] < 2**32, (M, N, K, kernel, units)
+        small = plan([(M, N, 128) for M in (1, 64, 2000) for N in range(8, 6000, 488)], out8)
+        assert all(g[0] for g in small)
+        assert [g[0] for g in plan([(1, 2**31 - 8, 8), (64, 2**31 - 256, 8), (2**31 - 1, 8, 8), (2**31 - 256, 4096, 256)], out8)] == [0] * 4
