@@ -404,7 +404,7 @@ int pab_quantized_layout(long long rows, int K, void *buffer, size_t bytes, pab_
  * y, padding columns included.  One launch on `hip_stream`.
  * PAB_EINVAL: rows < 1, K not a positive multiple of 8, a pitch that is too
  * small or no multiple of 16 bytes, NULL or misaligned pointers, unknown dtype,
- * more than 2^28 blocks.  PAB_EDEVICE: launch failed.
+ * 2^28 blocks or more.  PAB_EDEVICE: launch failed.
  */
 int pab_quantize(long long rows, int K, int dtype, const void *x, long long ldx, const pab_q8 *y, void *hip_stream);
 
@@ -412,7 +412,8 @@ int pab_quantize(long long rows, int K, int dtype, const void *x, long long ldx,
  * 8-bit rows to values, added to a residual stream: out = x + gate * y, with x
  * [rows, K] (row pitch ldx) or NULL for 0 and gate [K] or NULL for 1, all of
  * type dtype; computed in fp32 and rounded once.  out may be x.  One launch.
- * Errors as pab_quantize, and PAB_EINVAL for 2^31 chunks of 8 columns or more.
+ * Errors as pab_quantize (more than 2^28 blocks), and PAB_EINVAL for 2^31
+ * chunks of 8 columns or more.
  */
 int pab_dequantize(long long rows, int K, int dtype, const pab_q8 *y, const void *x, long long ldx, const void *gate, void *out,
                    long long ldo, void *hip_stream);

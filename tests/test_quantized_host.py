@@ -61,6 +61,14 @@ def test_quantize_and_dequantize_refuse(rows, K, dtype, x, ldx):
         assert status("pab_dequantize", rows, K, dtype, q8(), x, ldx, 0, OK, 1152, None) == pab.EINVAL
 
 
+def test_quantize_refuses_more_threads_than_a_grid_holds():
+    """2^28 blocks of 16 threads each are 2^32."""
+    y = q8(ld=256, ld_scale=4)
+    assert status("pab_quantize", 1 << 28, 128, 0, OK, 128, y, None) == pab.EINVAL
+    assert status("pab_quantize", 1 << 27, 256, 1, OK, 256, y, None) == pab.EINVAL
+    assert "too many" in pab.pab_last_error()
+
+
 def test_dequantize_refuses_more_than_its_index_holds():
     """2^31 chunks of 8 columns: the launch splits a chunk's number into row and column by a high product that is exact below that."""
     y = q8(ld=4096, ld_scale=32)
