@@ -468,6 +468,8 @@ int pab_mlp_compute_quantized(long long n_tok, int hidden, int inner, const void
  * scratch: pab_attention_quantized needs the bytes of one output tensor [T, S,
  * heads, head_dim] (16-byte aligned), pab_module_attention_quantized those of
  * pab_module_attention; needed on computed steps only.
+ * A slot has fewer than 2^28 blocks of 128 columns (34 GB): for larger ones
+ * pab_workspace_bytes_quantized is 0 and pab_create_quantized PAB_EINVAL.
  */
 size_t pab_workspace_bytes_quantized(const pab_config *cfg);
 int pab_create_quantized(const pab_config *cfg, void *workspace, size_t workspace_bytes, pab_ctx **out);

@@ -311,8 +311,11 @@ size_t slots_of(const pab_config &c) {
   return slots;
 }
 
-// a slot of 8-bit rows [T * S, heads * head_dim]
-size_t quantized_slot_bytes_of(const pab_config &c) { return pab::q8_bytes((long long)c.T * c.S, (long long)c.heads * c.head_dim); }
+// a slot of 8-bit rows [T * S, heads * head_dim]; 0: too large for the pass that fills it
+size_t quantized_slot_bytes_of(const pab_config &c) {
+  const long long tok = (long long)c.T * c.S, C = (long long)c.heads * c.head_dim;
+  return tok * ((C + 127) / 128) < pab::Q8_BLOCKS ? pab::q8_bytes(tok, C) : 0;
+}
 
 int create_context(const pab_config *cfg, void *workspace, size_t workspace_bytes, bool quantized, pab_ctx **out) {
   if (!out) return fail(PAB_EINVAL, "out is NULL");
@@ -322,7 +325,7 @@ int create_context(const pab_config *cfg, void *workspace, size_t workspace_byte
   if (!workspace) return fail(PAB_EINVAL, "workspace is NULL");
   if (reinterpret_cast<uintptr_t>(workspace) & 255u) return fail(PAB_EINVAL, "workspace must be 256-byte aligned");
   const size_t slot = quantized ? quantized_slot_bytes_of(*cfg) : slot_bytes_of(*cfg), need = slot * slots_of(*cfg);
-  if (!slot) return fail(PAB_EINVAL, "slots too large");
+  if (!slot) return fail(PAB_EINVAL, "slots of 8-bit rows hold fewer than 2^28 blocks");
   if (workspace_bytes < need)
     return fail(PAB_ENOMEM, "workspace has %zu bytes, the cache needs %zu", workspace_bytes, need);
   pab_ctx *ctx = new (std::nothrow) pab_ctx;
@@ -862,7 +865,9 @@ size_t pab_workspace_bytes(const pab_config *cfg) {
 
 size_t pab_workspace_bytes_quantized(const pab_config *cfg) {
   if (check_config(cfg) != PAB_OK) return 0;
-  return quantized_slot_bytes_of(*cfg) * slots_of(*cfg);
+  const size_t slot = quantized_slot_bytes_of(*cfg);
+  if (!slot) fail(PAB_EINVAL, "slots of 8-bit rows hold fewer than 2^28 blocks");
+  return slot * slots_of(*cfg);
 }
 
 int pab_create(const pab_config *cfg, void *workspace, size_t workspace_bytes, pab_ctx **out) {

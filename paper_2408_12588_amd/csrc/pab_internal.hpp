@@ -16,6 +16,8 @@ PAB_HIDDEN int fail(int code, const char *fmt, ...) __attribute__((format(printf
 
 inline bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
+// Blocks of 128 columns from which on a matrix is too large for the quantiser: 16 threads for each are 2^32, one more than a grid holds
+constexpr long long Q8_BLOCKS = 1LL << 28;
 // 8-bit rows of [rows, K] in one buffer, as pab_quantized_layout places them: bytes (0: too large), and the matrix at `buffer`
 PAB_HIDDEN size_t q8_bytes(long long rows, long long K);
 PAB_HIDDEN pab_q8 q8_at(void *buffer, long long rows, long long K);

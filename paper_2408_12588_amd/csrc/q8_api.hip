@@ -16,7 +16,6 @@ namespace {
 using pab::aligned16;
 using pab::fail;
 
-constexpr long long Q8_BLOCKS = 1LL << 28;   // the quantiser's 16 threads for each are as many as a grid holds, and one too many
 constexpr long long MAX_PITCH = 1LL << 24;   // bytes: 32-bit offsets inside a tile of up to 256 rows
 
 bool float_type(int dtype) { return dtype == PAB_BF16 || dtype == PAB_F32; }
@@ -45,7 +44,7 @@ int check_q8(const char *name, const pab_q8 *y, long long K) {
 int check_rows(long long rows, int K, int dtype) {
   if (!float_type(dtype)) return fail(PAB_EINVAL, "dtype %d is not bf16(0)/f32(1)", dtype);
   if (rows < 1 || K < 8 || K % 8) return fail(PAB_EINVAL, "rows=%lld must be >= 1, K=%d a positive multiple of 8", rows, K);
-  if (rows > (1LL << 31) || rows * blocks_of(K) > Q8_BLOCKS)
+  if (rows > (1LL << 31) || rows * blocks_of(K) > pab::Q8_BLOCKS)
     return fail(PAB_EINVAL, "%lld rows of %d are too many for one launch", rows, K);
   return PAB_OK;
 }
@@ -225,7 +224,7 @@ int quantize(long long rows, int K, int dtype, const void *x, long long ldx, con
   if ((rc = check_rows(rows, K, dtype)) != PAB_OK || (rc = check_pitch("x", x, ldx, K, dtype)) != PAB_OK ||
       (rc = check_q8("y", y, K)) != PAB_OK)
     return rc;
-  if (rows * blocks_of(K) >= Q8_BLOCKS) return fail(PAB_EINVAL, "%lld rows of %d are too many for one launch", rows, K);
+  if (rows * blocks_of(K) >= pab::Q8_BLOCKS) return fail(PAB_EINVAL, "%lld rows of %d are too many for one launch", rows, K);
   QuantizeParams p;
   p.x = x; p.ldx = ldx;
   p.data = static_cast<unsigned char *>(y->data); p.scale = static_cast<unsigned char *>(y->scale);

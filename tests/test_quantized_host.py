@@ -153,6 +153,21 @@ def test_contexts_do_not_mix():
         pab.lib.pab_destroy(h)
 
 
+def test_quantized_slots_are_what_a_launch_fills():
+    """A slot that the quantiser refuses is refused when the context is made, not behind the attention of its first computed step."""
+    big = pab.make_config(1, 1 << 14, 1 << 14, 0, 4, 32, pab.BF16, 6, (2, 0, 0), 1, 4)        # 2^28 rows of one block
+    fits = pab.make_config(1, 1 << 14, (1 << 14) - 1, 0, 4, 32, pab.BF16, 6, (2, 0, 0), 1, 4)
+    h = ctypes.c_void_p()
+    assert pab.lib.pab_workspace_bytes_quantized(ctypes.byref(big)) == 0 and "2^28" in pab.pab_last_error()
+    assert status("pab_create_quantized", ctypes.byref(big), OK, 1 << 50, ctypes.byref(h)) == pab.EINVAL and not h.value
+    with pytest.raises(pab.PabError):
+        pab.QuantizedContext(big)
+    need = pab.lib.pab_workspace_bytes_quantized(ctypes.byref(fits))
+    assert need == pab.pab_quantized_bytes(2**28 - 2**14, 128)
+    assert status("pab_create_quantized", ctypes.byref(fits), OK, need, ctypes.byref(h)) == pab.OK
+    pab.lib.pab_destroy(h)
+
+
 def test_quantized_context_refuses():
     cfg, s = config(), pab.pab_q8()
     h = context(pab.lib.pab_create_quantized, cfg)
