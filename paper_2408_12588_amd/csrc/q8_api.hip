@@ -104,17 +104,14 @@ int launch_product(const pab::GemmPlan &g, const pab::GemmQ8Params &p, hipStream
   return launched();
 }
 
-int product(int M, int N, int K, const pab_q8 *A, const pab_q8 *W, const void *bias, int act, void *C, long long ldc, const pab_q8 *C8,
-            hipStream_t st) {
-  if (M < 1 || N < 8 || N % 8 || K < 8 || K % 8)
-    return fail(PAB_EINVAL, "M=%d must be >= 1, N=%d and K=%d positive multiples of 8", M, N, K);
-  if (act != PAB_NONE && act != PAB_GELU) return fail(PAB_EINVAL, "activation %d is not none(0)/gelu(1)", act);
-  int rc;
-  if ((rc = check_q8("A", A, K)) != PAB_OK || (rc = check_q8("W", W, K)) != PAB_OK) return rc;
-  if (bias && !aligned16(bias)) return fail(PAB_EINVAL, "bias must be 16-byte aligned");
-  if (!C == !C8) return fail(PAB_EINVAL, "one of C and C8 must be given");
-  if (C && (rc = check_pitch("C", C, ldc, N, PAB_BF16)) != PAB_OK) return rc;
-  if (C8 && (rc = check_q8("C8", C8, N)) != PAB_OK) return rc;
+int plan_product(int M, int N, int K, bool out8, int act, pab::GemmPlan *g) {
+  *g = pab::plan_q8(M, N, (int)blocks_of(K), out8, act == PAB_GELU);
+  return g->kernel ? PAB_OK : fail(PAB_EINVAL, "M=%d N=%d: matrix too large for one launch", M, N);
+}
+
+// arguments checked, g from plan_product
+int launch_planned(const pab::GemmPlan &g, int M, int N, int K, const pab_q8 *A, const pab_q8 *W, const void *bias, int act, void *C, long long ldc,
+                   const pab_q8 *C8, hipStream_t st) {
   pab::GemmQ8Params p;
   p.A = static_cast<const unsigned char *>(A->data); p.sa = static_cast<const unsigned char *>(A->scale);
   p.W = static_cast<const unsigned char *>(W->data); p.sw = static_cast<const unsigned char *>(W->scale);
@@ -127,13 +124,27 @@ int product(int M, int N, int K, const pab_q8 *A, const pab_q8 *W, const void *b
     p.ld8 = C8->ld; p.ls8 = C8->ld_scale;
   }
   p.M = M; p.N = N; p.nk = (int)blocks_of(K);
-  const pab::GemmPlan g = pab::plan_q8(M, N, p.nk, C8 != nullptr, act == PAB_GELU);
-  if (!g.kernel) return fail(PAB_EINVAL, "M=%d N=%d: matrix too large for one launch", M, N);
   p.n_mt = g.n_mt; p.n_nt = g.n_nt; p.by_feature = g.by_feature; p.n_inner = g.by_feature ? g.n_mt : g.n_nt;
   p.ms_tail = g.ms_tail; p.n_units = g.n_units;
   p.past = C8 ? past_caches(g, M, C8->data, 128 * blocks_of(N), C8->ld) : past_caches(g, M, C, 2LL * N, 2 * ldc);
   if (C8) return act ? launch_product<pab::Q8_GELU, true>(g, p, st) : launch_product<pab::Q8_NONE, true>(g, p, st);
   return act ? launch_product<pab::Q8_GELU, false>(g, p, st) : launch_product<pab::Q8_NONE, false>(g, p, st);
+}
+
+int product(int M, int N, int K, const pab_q8 *A, const pab_q8 *W, const void *bias, int act, void *C, long long ldc, const pab_q8 *C8,
+            hipStream_t st) {
+  if (M < 1 || N < 8 || N % 8 || K < 8 || K % 8)
+    return fail(PAB_EINVAL, "M=%d must be >= 1, N=%d and K=%d positive multiples of 8", M, N, K);
+  if (act != PAB_NONE && act != PAB_GELU) return fail(PAB_EINVAL, "activation %d is not none(0)/gelu(1)", act);
+  int rc;
+  if ((rc = check_q8("A", A, K)) != PAB_OK || (rc = check_q8("W", W, K)) != PAB_OK) return rc;
+  if (bias && !aligned16(bias)) return fail(PAB_EINVAL, "bias must be 16-byte aligned");
+  if (!C == !C8) return fail(PAB_EINVAL, "one of C and C8 must be given");
+  if (C && (rc = check_pitch("C", C, ldc, N, PAB_BF16)) != PAB_OK) return rc;
+  if (C8 && (rc = check_q8("C8", C8, N)) != PAB_OK) return rc;
+  pab::GemmPlan g;
+  if ((rc = plan_product(M, N, K, C8 != nullptr, act, &g)) != PAB_OK) return rc;
+  return launch_planned(g, M, N, K, A, W, bias, act, C, ldc, C8, st);
 }
 
 // ---- layernorm + modulate into 8-bit rows ----
@@ -301,12 +312,16 @@ int pab_mlp_compute_quantized(long long n_tok, int hidden, int inner, const void
   int rc;   // everything is checked before the first launch
   if ((rc = check_q8("w1", &w->w1, hidden)) != PAB_OK || (rc = check_q8("w2", &w->w2, inner)) != PAB_OK) return rc;
   if (!aligned16(w->b1) || !aligned16(w->b2)) return fail(PAB_EINVAL, "b1 and b2 must be 16-byte aligned");
+  pab::GemmPlan up, down;
+  if ((rc = plan_product((int)n_tok, inner, hidden, true, PAB_GELU, &up)) != PAB_OK ||
+      (rc = plan_product((int)n_tok, hidden, inner, false, PAB_NONE, &down)) != PAB_OK)
+    return rc;
   const hipStream_t st = static_cast<hipStream_t>(hip_stream);
   const pab_q8 h = pab::q8_at(scratch, n_tok, hidden);
   const pab_q8 u = pab::q8_at(static_cast<unsigned char *>(scratch) + pab::q8_bytes(n_tok, hidden), n_tok, inner);
   if ((rc = ln_modulate_q8((int)n_tok, hidden, x, w->shift, w->scale, h, st)) != PAB_OK) return rc;
-  if ((rc = product((int)n_tok, inner, hidden, &h, &w->w1, w->b1, PAB_GELU, nullptr, 0, &u, st)) != PAB_OK) return rc;
-  return product((int)n_tok, hidden, inner, &u, &w->w2, w->b2, PAB_NONE, out, hidden, nullptr, st);
+  if ((rc = launch_planned(up, (int)n_tok, inner, hidden, &h, &w->w1, w->b1, PAB_GELU, nullptr, 0, &u, st)) != PAB_OK) return rc;
+  return launch_planned(down, (int)n_tok, hidden, inner, &u, &w->w2, w->b2, PAB_NONE, out, hidden, nullptr, st);
 }
 
 long long pab_rope_factors_count(const int places[3], const int axis_dim[3]) {

@@ -119,6 +119,16 @@ def test_mlp_refuses():
         assert call(w=w) == pab.EINVAL, kw
 
 
+def test_mlp_refuses_products_that_no_launch_holds():
+    """... before its layernorm is launched: the status is a refusal also where there is no device."""
+    n, C, F = 2**25, 1152, 2**20 + 32
+    w = pab.pab_mlp_weights_quantized(OK, OK, q8(), 0, q8(ld=2**20 + 128, ld_scale=8196), 0)
+    need = pab.pab_mlp_scratch_bytes_quantized(n, C, F)
+    assert need
+    assert status("pab_mlp_compute_quantized", n, C, F, OK, w, OK, need, OK, None) == pab.EINVAL
+    assert "too large" in pab.pab_last_error()
+
+
 def config(dtype=pab.BF16, interval=(2, 2, 2)):
     return pab.make_config(2, 4, 8, 16, 4, 32, dtype, 6, interval, 1, 4)
 
