@@ -138,12 +138,15 @@ __global__ __launch_bounds__(256) void qk_norm_axes_kernel(const QkAxesParams p)
         float o[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) o[e] = v[w][e] * rstd * weight[w][0][e] + weight[w][1][e];
+        // What lies behind the last section is left alone, by selection: (1, 0) would make a NaN of an infinity's neighbour.  Costs 1 % (47.9 -> 48.4);
+        // with a branch for lanes that turn all of their pairs nothing, but 5 % where sections are not whole fours of pairs.
         if (turn) {
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             const float c = f[e][0], s = f[e][1], x = o[2 * e], y = o[2 * e + 1];
-            o[2 * e] = x * c - y * s;
-            o[2 * e + 1] = x * s + y * c;
+            const bool turned = 4 * part + e < p.end_x;
+            o[2 * e] = turned ? x * c - y * s : x;
+            o[2 * e + 1] = turned ? x * s + y * c : y;
           }
         }
         store_row8(static_cast<T *>(w ? p.k_out : p.q_out) + (w ? tok * p.ld_k_out : tok * p.ld_q_out) + head * D + 8 * part, o);

@@ -113,6 +113,35 @@ def test_rows_without_spread_or_finite_values():
             assert float(out[1, 0].abs().max()) <= 2e-3 and float(out[2, 1].abs().max()) == 0.0
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("D,dims", [(72, (8, 8, 8)), (72, (2, 14, 6)), (32, (0, 10, 0)), (128, (56, 0, 16)), (64, (0, 0, 0))])
+def test_what_is_not_turned_keeps_its_value(D, dims, dtype):
+    """Behind the last section nothing meets its neighbour: infinities and NaNs stay where they are, and the bits are those of a call
+    without a table."""
+    end, inf = sum(dims), float("inf")
+    q = normal(5, 6, 3, D).to(dtype)
+    q[0, 0, end], q[1, 1, end + 1], q[2, 2, D - 1], q[3, 0, D - 2] = inf, -inf, inf, float("nan")
+    q[4, 1, end:] = -0.0
+    places = (1, 3, 2)
+    f = pab.pab_rope_factors(places, dims, device=DEV)
+    out, _ = pab.pab_qk_norm_rope(q.to(DEV), None, places, dims, f, pab.NORM_NONE)
+    plain, _ = pab.pab_qk_norm_rope(q.to(DEV), None, places, dims, None, pab.NORM_NONE)
+    bits = torch.int16 if dtype == torch.bfloat16 else torch.int32
+    out, plain = out.cpu(), plain.cpu()
+    finite = q.isfinite()
+    assert torch.equal(out.isfinite(), finite)
+    same = finite[..., end:]
+    assert torch.equal(out[..., end:].contiguous().view(bits)[same], plain[..., end:].contiguous().view(bits)[same])
+    assert torch.equal(out[..., end:][~same & ~q[..., end:].isnan()], q[..., end:][~same & ~q[..., end:].isnan()])
+    gamma = torch.full((D,), 3e38).to(dtype)                  # products that overflow behind the section
+    gamma[:end] = 1.0
+    q = normal(6, 6, 3, D).to(dtype)
+    q[..., end::2], q[..., end + 1::2] = 4.0, 0.25
+    out, _ = pab.pab_qk_norm_rope(q.to(DEV), None, places, dims, f, pab.NORM_NONE, gamma_q=gamma.to(DEV))
+    out = out.cpu()
+    assert bool(out[..., end::2].isinf().all()) and bool(out[..., end + 1::2].isfinite().all()) and bool(out[..., :end].isfinite().all())
+
+
 def test_factors_of_far_and_stretched_places():
     """fp64 until the last rounding: 2^-24 of at most 1, and 10^-9 for an angle of 10^6 whose frequency is 10^-15 off."""
     places, dims = (300, 5, 64), (24, 32, 72)
