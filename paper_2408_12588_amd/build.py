@@ -52,8 +52,8 @@ def build_lib(verbose: bool = False, extra_flags=()) -> str:
     try:
         if failed:
             raise RuntimeError("hipcc failed building libpab.so")
-        res = subprocess.run([hipcc, "--offload-arch=gfx950", "-shared", "-o", tmp] + objects, stdout=subprocess.PIPE,
-                             stderr=subprocess.STDOUT, text=True)
+        res = subprocess.run([hipcc, "--offload-arch=gfx950", "-shared"] + list(extra_flags) + ["-o", tmp] + objects,
+                             stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
         if res.returncode != 0:
             sys.stderr.write(res.stdout + "\n")
             raise RuntimeError("hipcc failed linking libpab.so")
