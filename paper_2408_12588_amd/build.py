@@ -30,27 +30,33 @@ HIPCC_FLAGS = [
 ]
 
 
+def _compile(action, outputs, extra_flags, verbose=False) -> bool:
+    """Every source with its flags, all at once, into the files of `outputs`."""
+    hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
+    jobs = []
+    for src, out in zip(SOURCES + SOURCES_NAN, outputs):
+        dropped = ("-shared", "-fno-honor-nans") if src in SOURCES_NAN else ("-shared",)
+        cmd = [hipcc] + [f for f in HIPCC_FLAGS if f not in dropped] + list(extra_flags) + list(action) + ["-o", out, src]
+        if verbose:
+            print(" ".join(cmd), flush=True)
+        jobs.append(subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True))
+    done = True
+    for job in jobs:
+        text = "\n".join(l for l in job.communicate()[0].splitlines() if "packed-fp32-ops" not in l)
+        if job.returncode != 0:
+            sys.stderr.write(text + "\n")
+            done = False
+        elif verbose and text.strip():
+            print(text)
+    return done
+
+
 def build_lib(verbose: bool = False, extra_flags=()) -> str:
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
     tmp = LIB + ".tmp.%d" % os.getpid()
-    jobs, objects = [], []
-    for sources, flags in ((SOURCES, HIPCC_FLAGS), (SOURCES_NAN, [f for f in HIPCC_FLAGS if f != "-fno-honor-nans"])):
-        for src in sources:
-            objects.append("%s.%s.o" % (tmp, os.path.basename(src)))
-            cmd = [hipcc] + [f for f in flags if f != "-shared"] + list(extra_flags) + ["-c", "-o", objects[-1], src]
-            if verbose:
-                print(" ".join(cmd), flush=True)
-            jobs.append((cmd, subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)))
-    failed = False
-    for cmd, job in jobs:
-        out = "\n".join(l for l in job.communicate()[0].splitlines() if "packed-fp32-ops" not in l)
-        if job.returncode != 0:
-            sys.stderr.write(out + "\n")
-            failed = True
-        elif verbose and out.strip():
-            print(out)
+    objects = ["%s.%s.o" % (tmp, os.path.basename(src)) for src in SOURCES + SOURCES_NAN]
     try:
-        if failed:
+        if not _compile(["-c"], objects, extra_flags, verbose):
             raise RuntimeError("hipcc failed building libpab.so")
         res = subprocess.run([hipcc, "--offload-arch=gfx950", "-shared"] + list(extra_flags) + ["-o", tmp] + objects,
                              stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
@@ -115,14 +121,19 @@ def ensure_built() -> str:
 
 
 def device_asm(path: str, extra_flags=()) -> str:
-    """Write the gfx950 assembly of the device code (same flags as the library) to `path`."""
-    hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
-    flags = [f for f in HIPCC_FLAGS if f not in ("-shared", "-fPIC")]
-    cmd = [hipcc] + flags + list(extra_flags) + ["-S", "--cuda-device-only", "-o", path] + SOURCES
-    res = subprocess.run(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
-    if res.returncode != 0:
-        sys.stderr.write(res.stdout + "\n")
-        raise RuntimeError("hipcc failed writing the device assembly")
+    """Write the gfx950 assembly of the device code of every source (same flags as the library) to `path`, one after the other."""
+    parts = ["%s.%s" % (path, os.path.basename(src)) for src in SOURCES + SOURCES_NAN]
+    try:
+        if not _compile(["-S", "--cuda-device-only"], parts, extra_flags):
+            raise RuntimeError("hipcc failed writing the device assembly")
+        with open(path, "w") as f:
+            for part in parts:
+                with open(part) as g:
+                    f.write(g.read())
+    finally:
+        for part in parts:
+            if os.path.exists(part):
+                os.unlink(part)
     return path
 
 

@@ -33,3 +33,13 @@ def test_extra_flags_reach_every_step(tmp_path, monkeypatch):
     assert all(a[a.index("-Xsome") + 1] == "--flag" for a in got)
     assert all("-packed-fp32-ops" in a for a in compiled)
     assert os.listdir(tmp_path).count("libpab.so") == 1 and not [f for f in os.listdir(tmp_path) if f.endswith(".o")]
+
+
+def test_assembly_is_of_every_source(tmp_path, monkeypatch):
+    """... so that what is held of the generated code is held of all kernels, compiled as they are for the library."""
+    path = str(tmp_path / "out" / "pab.s")
+    os.mkdir(tmp_path / "out")
+    got = calls(tmp_path, monkeypatch, lambda: pab_build.device_asm(path, ["--flag"]))
+    assert sorted(a[-1] for a in got) == sorted(pab_build.SOURCES + pab_build.SOURCES_NAN)
+    assert all("-S" in a and "--flag" in a and ("-fno-honor-nans" in a) == (a[-1] in pab_build.SOURCES) for a in got)
+    assert os.listdir(tmp_path / "out") == ["pab.s"]
