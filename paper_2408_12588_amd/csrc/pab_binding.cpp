@@ -191,8 +191,9 @@ struct Rows {
 
 // whether these tensors hold 8-bit rows of K columns
 bool rows_in(const at::Tensor &d, const at::Tensor &s, long long K, Rows *r) {
-  if (d.dim() != 2 || s.dim() != 2 || d.element_size() != 1 || s.element_size() != 1 || d.size(0) != s.size(0) || d.size(0) < 1 || K < 1 ||
-      K > 0x7fffff00 || d.get_device() != s.get_device())
+  const auto dt = d.scalar_type(), st = s.scalar_type();
+  if ((dt != at::kByte && dt != at::kFloat8_e4m3fn) || (st != at::kByte && st != at::kFloat8_e8m0fnu) || d.dim() != 2 || s.dim() != 2 ||
+      d.size(0) != s.size(0) || d.size(0) < 1 || K < 1 || K > 0x7fffff00 || d.get_device() != s.get_device())
     return false;
   const long long nb = (K + 127) / 128;
   if (d.size(1) < 128 * nb || s.size(1) < nb || d.stride(1) != 1 || s.stride(1) != 1) return false;

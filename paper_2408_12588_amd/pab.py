@@ -635,7 +635,7 @@ def _new(shape, dtype, device, stream):
 
 
 class Q8:
-    """8-bit rows: ``data`` [rows, >= K rounded up to 128] (uint8 or e4m3), ``scale`` [rows, ...] exponent bytes (uint8), device
+    """8-bit rows: ``data`` [rows, >= K rounded up to 128] (uint8 or e4m3), ``scale`` [rows, ...] exponent bytes (uint8 or e8m0), device
     tensors that this object keeps; ``K`` columns of values."""
     __slots__ = ("data", "scale", "K")
 
@@ -643,7 +643,9 @@ class Q8:
         self.data, self.scale, self.K = data, scale, K
         if _binding.q8_ok(data, scale, K) is True:
             return
-        if data.dim() != 2 or scale.dim() != 2 or data.element_size() != 1 or scale.element_size() != 1:
+        if data.dtype not in (torch.uint8, torch.float8_e4m3fn) or scale.dtype not in (torch.uint8, torch.float8_e8m0fnu):
+            raise ValueError("data must be uint8 or e4m3, scale uint8 or e8m0, not %s and %s" % (data.dtype, scale.dtype))
+        if data.dim() != 2 or scale.dim() != 2:
             raise ValueError("data and scale are matrices of bytes")
         if not data.is_cuda or not scale.is_cuda:
             raise ValueError("libpab takes device tensors")

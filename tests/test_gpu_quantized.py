@@ -132,6 +132,18 @@ def test_residual(dtype, eps, rows, K, gated):
     assert torch.equal(same, out) and torch.equal(base[:, 0], kept[:, 0]) and torch.equal(base[:, 1, K:], kept[:, 1, K:])
 
 
+def test_types_of_the_bytes():
+    """The named types are the same bytes; bytes of another meaning are refused, also of device tensors."""
+    y, values = make_q8(normal(4, 3, 136))
+    named = pab.Q8(y.data.view(torch.float8_e4m3fn), y.scale.view(torch.float8_e8m0fnu), 136)
+    assert np.array_equal(pab.pab_dequantize(named, dtype=torch.float32).cpu().double().numpy(), values)
+    for other in (torch.float8_e5m2, torch.float8_e4m3fnuz, torch.int8):
+        with pytest.raises(ValueError):
+            pab.Q8(y.data.view(other), y.scale, 136)
+    with pytest.raises(ValueError):
+        pab.Q8(y.data, y.scale.view(torch.int8), 136)
+
+
 # ---- products ----
 def eights(values, scale, K):
     """Largest magnitude of every eight columns, not below the smallest normal value 2^-6 of its block where it is not zero."""

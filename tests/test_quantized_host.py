@@ -254,6 +254,15 @@ def test_python_checks_its_tensors():
             f()
 
 
+@pytest.mark.parametrize("data,scale", [("float8_e5m2", "uint8"), ("float8_e4m3fnuz", "uint8"), ("float8_e8m0fnu", "uint8"), ("int8", "uint8"),
+                                        ("bool", "uint8"), ("uint8", "int8"), ("uint8", "float8_e4m3fn"), ("float32", "uint8")])
+def test_other_bytes_are_no_rows(data, scale):
+    """Bytes of another meaning would be read as e4m3 values and powers of two."""
+    import torch
+    with pytest.raises(ValueError, match="uint8 or e4m3"):
+        pab.Q8(torch.zeros(4, 128, dtype=torch.uint8).to(getattr(torch, data)), torch.zeros(4, 4, dtype=torch.uint8).view(getattr(torch, scale)), 128)
+
+
 def test_mlp_weights_are_on_one_device():
     import torch
 
