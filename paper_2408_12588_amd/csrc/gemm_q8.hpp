@@ -27,7 +27,7 @@ struct GemmQ8Params {
   int n_mt, n_nt;                    // token / feature tiles
   int by_feature, n_inner;           // consecutive tiles share their features (1) or their tokens (0), n_inner of them
   int ms_tail, n_units;              // large tiles: see gemm_q8_stream.hpp
-  int past;                          // the output goes past the caches
+  int past;                          // the output goes past the caches (8-bit rows: of large tiles only)
 };
 
 enum { Q8_NONE = 0, Q8_GELU = 1 };
@@ -286,7 +286,8 @@ __global__ __launch_bounds__(64 * WM * WN * KG, KG > 1 ? WM * WN * KG / 4 : 2) v
       for (int i = 0; i < (16 * CPR + 63) / 64; ++i) {
         const int row = 64 / CPR * i + lane / CPR, mr = mw + 16 * a + row;
         if (row < 16 && mr < M && (fw & ~127) < N)         // a block that has a column is written whole
-          put16(p.C8 + mr * p.ld8 + fw + 16 * (lane % CPR), *(const __attribute__((address_space(3))) u32x4 *)(size_t)(xs + SEG * row + 16 * (lane % CPR)), p.past);
+          *reinterpret_cast<u32x4 *>(p.C8 + mr * p.ld8 + fw + 16 * (lane % CPR)) =
+              *(const __attribute__((address_space(3))) u32x4 *)(size_t)(xs + SEG * row + 16 * (lane % CPR));
       }
       __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     }

@@ -14,7 +14,7 @@
 // Between tiles: the first slice of a tile, written out by itself, starts the sums from the bias, which was copied a tile ahead; its barrier does not
 // wait for the stores of the tile before (memory operations of a wavefront end in order, so leaving as many of the last ones open as
 // there were stores is enough); and the stores of a step of the epilogue go out behind the arithmetic of the next.  Large outputs are written past
-// the caches (q8_api.hip says when): what all workgroups of an XCD store at once is as large as its L2, and drives out the operands.  The 32-byte
+// the caches (q8_plan.hpp says when): what all workgroups of an XCD store at once is as large as its L2, and drives out the operands.  The 32-byte
 // pieces of odd sub-tiles never are: memory would read what it keeps of them (288-feature tiles, 53536 x 3584 x 200: 92 -> 135).
 //
 // Measured, us: a slice of 256 x 256 x 128 takes 1.58, of 256 x 288 1.70, and a tile 3 (8-bit or large outputs) to 5 and 8 more, with GELU 3 more.

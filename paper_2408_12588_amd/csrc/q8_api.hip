@@ -57,17 +57,6 @@ int check_pitch(const char *name, const void *p, long long ld, long long K, int 
 }
 
 // ---- products ----
-// Whether an output of M rows of `width` bytes, `pitch` apart, is written past the caches.  Only in whole pieces of 64 bytes, or memory reads what it
-// keeps of them (53536 x 3544 x 200: 138 -> 252 us).  The kernels with a tile per workgroup always gain (4413 x 1152 x 1152 12.2 -> 11.4, with the pass
-// that reads the output 18.5 -> 17.1).  Large tiles, whose operands wait in L2 while a tile is stored, gain more, but what reads a small output finds it in
-// the last-level cache of 256 MB otherwise, so theirs must be large: 65536 x 4096 x 512 (537 MB) 198 -> 148, 25440 x 3456 x 1152 (176 MB) 109 -> 97,
-// with the norm that reads it 146 -> 139, but 25440 x 1152 x 1152 (59 MB) with the pass that reads it 49.5 -> 54, the two products of an MLP with 117 MB of
-// 8-bit rows between them 283 -> 291.
-bool past_caches(const pab::GemmPlan &g, long long M, const void *to, long long width, long long pitch) {
-  if ((reinterpret_cast<uintptr_t>(to) | (unsigned long long)width | (unsigned long long)pitch) % 64) return false;
-  return g.kernel >= 64 || M * width > (150LL << 20);
-}
-
 template <int ACT, bool OUT8>
 int launch_product(const pab::GemmPlan &g, const pab::GemmQ8Params &p, hipStream_t st) {
   const dim3 persistent((unsigned)std::min(g.n_units, pab::GEMM_CUS)), tiles((unsigned)((g.n_units + 7) / 8 * 8));
@@ -126,7 +115,8 @@ int launch_planned(const pab::GemmPlan &g, int M, int N, int K, const pab_q8 *A,
   p.M = M; p.N = N; p.nk = (int)blocks_of(K);
   p.n_mt = g.n_mt; p.n_nt = g.n_nt; p.by_feature = g.by_feature; p.n_inner = g.by_feature ? g.n_mt : g.n_nt;
   p.ms_tail = g.ms_tail; p.n_units = g.n_units;
-  p.past = C8 ? past_caches(g, M, C8->data, 128 * blocks_of(N), C8->ld) : past_caches(g, M, C, 2LL * N, 2 * ldc);
+  p.past = C8 ? pab::q8_past_caches(g.kernel, true, M, C8->data, 128 * blocks_of(N), C8->ld)
+              : pab::q8_past_caches(g.kernel, false, M, C, 2LL * N, 2 * ldc);
   if (C8) return act ? launch_product<pab::Q8_GELU, true>(g, p, st) : launch_product<pab::Q8_NONE, true>(g, p, st);
   return act ? launch_product<pab::Q8_GELU, false>(g, p, st) : launch_product<pab::Q8_NONE, false>(g, p, st);
 }

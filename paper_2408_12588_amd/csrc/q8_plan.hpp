@@ -12,6 +12,7 @@
 // Against the best kernel of each of 1200 random shapes the choice loses 0.7 % in the mean.
 #pragma once
 #include <algorithm>
+#include <cstdint>
 
 #include "launch_plan.hpp"
 
@@ -60,6 +61,20 @@ inline GemmPlan plan_q8(int M, int N, int nk, bool out8, bool gelu) {
   if (!out8) plan_stream(9, M, N, nk, 1.70 * nk + 8.0, 0.34, &best);
   if (best.n_units > Q8_MOST) best.kernel = 0;
   return best;
+}
+
+// Whether an output of M rows of `width` bytes, `pitch` apart, is written past the caches.  Only where rows start at whole pieces of 64 bytes, or memory
+// reads what it keeps of them (53536 x 3544 x 200: 138 -> 252 us).  In us, through the caches / past them, alone and with the pass or product that reads it:
+//   a tile per workgroup, bf16: gains (4413 x 1152 x 1152 12.2 / 11.2 and 16.5 / 16.1, 2600 x 2304 x 1152 12.5 / 11.2 and 17.3 / 16.7)
+//   a tile per workgroup, 8-bit rows: the next product reads them, many times over, and two of the kernels (96, 97) write them 32 bytes at a time: through
+//   the caches (1260 x 3456 x 576 9.1 / 8.9 but 22.1 / 25.3, 2600 x 2304 x 2304 20.3 / 20.3 and 32.9 / 35.4, MLP of 501 x 1152 / 4608 25.6 / 28.8;
+//   6249 x 576 x 1152 19.7 / 19.1 is the largest loss)
+//   large tiles, whose operands wait in L2 while a tile is stored: large outputs gain (25440 x 3456 x 1152, 176 MB, 116 / 95 and 157 / 151; in rows
+//   40000 x 4608 x 1152 207 / 189 and 425 / 427), of a small one the reader finds more in the last-level cache of 256 MB (25440 x 1152 x 1152, 59 MB, 41.4 / 40.2
+//   but 56.9 / 58.1; in rows 25440 x 4608 x 1152, 117 MB, 134 / 124 but 275 / 279); bf16 between 100 and 150 MB would gain (19000 x 3456 x 1152 89 / 72 and 117 / 115)
+inline bool q8_past_caches(int kernel, bool out8, long long M, const void *to, long long width, long long pitch) {
+  if ((reinterpret_cast<uintptr_t>(to) | (unsigned long long)width | (unsigned long long)pitch) % 64) return false;
+  return kernel >= 64 ? !out8 : M * width > (150LL << 20);
 }
 
 }  // namespace pab

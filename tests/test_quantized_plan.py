@@ -111,3 +111,31 @@ def test_launches_have_fewer_threads_than_a_grid_holds(plan):
         small = plan([(M, N, 128) for M in (1, 64, 2000) for N in range(8, 6000, 488)], out8)
         assert all(g[0] for g in small)
         assert [g[0] for g in plan([(1, 2**31 - 8, 8), (64, 2**31 - 256, 8), (2**31 - 1, 8, 8), (2**31 - 256, 4096, 256)], out8)] == [0] * 4
+
+
+def test_outputs_past_the_caches(tmp_path):
+    """bf16 outputs of a tile per workgroup always, their 8-bit rows never (some wavefronts write 32 bytes of a row, and the next product reads all of
+    it), large tiles' from 150 MB on; nothing whose rows do not start at multiples of 64 bytes."""
+    (tmp_path / "past.cpp").write_text(r'''
+#include <cstdio>
+#include "q8_plan.hpp"
+int main() {
+  int kernel, out8; long long M, to, width, pitch;
+  while (scanf("%d %d %lld %lld %lld %lld", &kernel, &out8, &M, &to, &width, &pitch) == 6)
+    printf("%d\n", pab::q8_past_caches(kernel, out8, M, reinterpret_cast<void *>(to), width, pitch));
+}
+''')
+    exe = str(tmp_path / "past")
+    subprocess.run(["g++", "-std=c++17", "-O1", "-Wall", "-I", CSRC, "-o", exe, str(tmp_path / "past.cpp")], check=True, timeout=120)
+
+    def ask(*rows):
+        out = subprocess.run([exe], input="".join("%d %d %d %d %d %d\n" % r for r in rows), capture_output=True, text=True, check=True, timeout=60).stdout
+        return [bool(int(x)) for x in out.split()]
+
+    at = 1 << 20
+    tiles = sorted((TO_ROWS | TO_VALUES) - {8, 9, 16, 32, 48})
+    assert all(ask(*((k, 0, M, at, 2304, 2304) for k in tiles for M in (1, 65, 10**6))))
+    assert not any(ask(*((k, 1, M, at, 1152, 1152) for k in tiles for M in (1, 65, 10**6))))
+    assert ask((8, 0, 25440, at, 6912, 6912), (9, 0, 57600, at, 2304, 2304), (8, 0, 25440, at, 2304, 2304), (8, 1, 25440, at, 4608, 4608),
+               (8, 1, 40000, at, 4608, 4608)) == [True, False, False, False, True]
+    assert not any(ask(*((k, 0, 10**6, a, w, p) for k in tiles + [8, 9] for a, w, p in ((at + 16, 2304, 2304), (at, 2320, 2304), (at, 2304, 2320)))))
