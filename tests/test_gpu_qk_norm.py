@@ -177,6 +177,42 @@ def test_many_tokens_in_order():
     assert torch.equal(out.cpu()[:, 0], torch.cat(parts, 1))
 
 
+@pytest.mark.parametrize("dtype,groups", [(torch.bfloat16, 1536), (torch.float32, 8192)])
+@pytest.mark.parametrize("D,dims", [(32, (8, 12, 12)), (64, (16, 24, 24)), (72, (24, 24, 24)), (96, (32, 32, 20)), (128, (16, 56, 56))])
+def test_wavefronts_take_several_groups_of_rows(D, dims, dtype, groups):
+    """More (token, head) rows than `groups` workgroups of four wavefronts hold at 64 / (D / 8) rows each, up to which every wavefront has one group: each takes
+    two, some a third, the last one part of a group.  Every element against the definition in fp64 (vectorised, on the device), with check's tolerance."""
+    places, batch, Hq, Hk = (3, 7, 11), 2, 4, 3
+    at_once = groups * 4 * (64 // (D // 8))
+    T = -(-(2 * at_once + 4 * 64) // (batch * 77 * Hq))
+    places = (T, 7, 11)
+    n = batch * T * 77
+    assert 2 * at_once < n * Hq < 3 * at_once
+    gen = torch.Generator(device=DEV).manual_seed(D)
+    g = [t.to(DEV) for t in weights(D, dtype, 70)]
+    f = pab.pab_rope_factors(places, dims, device=DEV)
+    q, k = ((torch.randn(n, h, D, generator=gen, device=DEV) * 2 + 0.5).to(dtype) for h in (Hq, Hk))
+    got = pab.pab_qk_norm_rope(q, k, places, dims, f, pab.NORM_LAYER, *g, eps=1e-6)
+    table = torch.from_numpy(qo.rope_factors(places, dims)).to(DEV)
+    token = torch.arange(n, device=DEV) % (T * 77)
+    columns, first = [], 0
+    for place, m, d in zip((token // 77, token // 11 % 7, token % 11), places, dims):
+        columns.append(table[first:first + m * (d // 2)].view(m, d // 2, 2)[place])
+        first += m * (d // 2)
+    turn = torch.cat(columns, 1)[:, None]
+    r = 2 * turn.shape[2]
+    for out, x, gamma, beta in ((got[0], q, *g[:2]), (got[1], k, *g[2:])):
+        v = x.double()
+        mean = v.mean(-1, keepdim=True)
+        sigma = torch.sqrt(v.var(-1, unbiased=False, keepdim=True) + 1e-6)
+        v = (v - mean) / sigma * gamma.double() + beta.double()
+        big = (v.abs().amax(-1, keepdim=True) + mean.abs() / sigma) * (1 + gamma.double().abs().max())
+        a, b = v[..., 0:r:2], v[..., 1:r:2]
+        want = torch.cat([torch.stack([a * turn[..., 0] - b * turn[..., 1], a * turn[..., 1] + b * turn[..., 0]], -1).flatten(-2), v[..., r:]], -1)
+        over = (out.double() - want).abs() - HALF[dtype] * want.abs() - (D + 16) * 2.0 ** -23 * big
+        assert bool((over <= 0).all()), float(over.max())
+
+
 def test_streams_and_graphs():
     places, dims = (4, 5, 6), (24, 24, 24)
     q, k = normal(7, 120, 16, 72).bfloat16().to(DEV), normal(8, 120, 16, 72).bfloat16().to(DEV)

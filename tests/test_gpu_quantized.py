@@ -377,6 +377,41 @@ def test_mlp(n, C, F):
     assert np.linalg.norm(got - want) <= (BF + 0.0025) * np.linalg.norm(want)
 
 
+MLP_STAGES = [(1, 32, 32), (5, 160, 96), (64, 1152, 4608), (130, 576, 2304), (300, 800, 1600), (257, 2048, 1056), (1260, 576, 2304), (25440, 1152, 4608)]
+
+
+@pytest.mark.parametrize("n,C,F", MLP_STAGES)
+def test_mlp_stage_by_stage(n, C, F):
+    """What each launch leaves, element by element against the definition of that stage on what the launch before it left (8-bit rows in the scratch
+    buffer: those of layernorm + modulate, then those between the products), so that nothing is hidden by the norm of a whole output.  Some rows of the
+    largest, all of the others.  Layernorm: fp32 sums over C, at most C 2^-24 of their terms off, and a handful of steps, relative to the row's
+    largest normed value and to what the mean takes away: (C + 16) 2^-23 of that."""
+    gen = torch.Generator(device=DEV).manual_seed(n + C)
+    x = (torch.randn(n, C, generator=gen, device=DEV) * 2 + 0.5).bfloat16()
+    shift, scale = (0.1 * normal(1, C)).bfloat16(), (0.1 * normal(2, C)).bfloat16()
+    b1, b2 = normal(3, F).bfloat16(), normal(4, C).bfloat16()
+    (w1, v1), (w2, v2) = make_q8(normal(5, F, C) / C ** 0.5), make_q8(normal(6, C, F) / F ** 0.5)
+    w = pab.mlp_weights_quantized(shift.to(DEV), scale.to(DEV), w1, b1.to(DEV), w2, b2.to(DEV))
+    scratch = torch.full((pab.pab_mlp_scratch_bytes_quantized(n, C, F),), 0x7F, dtype=torch.uint8, device=DEV)
+    out = pab.pab_mlp_compute_quantized(x, w, scratch=scratch)
+    rows = np.arange(n) if n <= 300 else np.unique(np.concatenate([np.arange(0, n, n // 120), np.arange(n - 70, n), np.arange(250, 260)]))
+    first = pab.pab_quantized_bytes(n, C)
+    whole = [pab.q8_view(scratch[:first], n, C), pab.q8_view(scratch[first:], n, F)]
+    h, u = (pab.Q8(y.data[rows], y.scale[rows], y.K) for y in whole)
+    xf, f64 = x[rows].cpu().double().numpy(), lambda t: t.double().numpy()   # noqa: E731
+    straight = qo.layer_norm(xf)
+    big = np.abs(straight).max(-1, keepdims=True) + np.abs(xf.mean(-1, keepdims=True)) / np.sqrt(xf.var(-1, keepdims=True) + 1e-6)
+    want = straight * (1 + f64(scale)) + f64(shift)
+    check_rows_near(h, want, (C + 16) * 2.0 ** -23 * (big * (1 + np.abs(f64(scale)).max()) + np.abs(f64(shift)).max()), C)
+    hv = qo.dequantize(*rows_of(h), C)
+    plain = qo.linear(hv, v1, f64(b1))
+    tol = 1.13 * product_tolerance(h, hv, w1, v1, np.abs(f64(b1))) + 2.0 ** -18 * np.abs(plain) + 1e-30
+    check_rows_near(u, qo.gelu(plain), tol, F)
+    uv = qo.dequantize(*rows_of(u), F)
+    want, tol = qo.linear(uv, v2, f64(b2)), product_tolerance(u, uv, w2, v2, np.abs(f64(b2)))
+    assert np.all(np.abs(out[rows].cpu().double().numpy() - want) <= BF * np.abs(want) + tol * (1 + BF))
+
+
 def test_mlp_keeps_its_rows():
     """A token's output does not depend on the others, scratch content does not matter."""
     x, w, _ = mlp_case(300, 576, 1152, 3)

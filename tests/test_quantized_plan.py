@@ -113,6 +113,12 @@ def test_launches_have_fewer_threads_than_a_grid_holds(plan):
         assert [g[0] for g in plan([(1, 2**31 - 8, 8), (64, 2**31 - 256, 8), (2**31 - 1, 8, 8), (2**31 - 256, 4096, 256)], out8)] == [0] * 4
 
 
+def test_tested_mlps_reach_every_family(plan):
+    """Products of an MLP by tiles of one and of several K groups, and both by large tiles, as the largest runs do."""
+    chains = [(plan([(n, F, C)], 1, 1)[0][0], plan([(n, C, F)], 0)[0][0]) for n, C, F in G.MLP_STAGES]
+    assert chains[-1] == (8, 8) and {up for up, _ in chains} >= {8, 96, 97} and {down for _, down in chains} >= {8, 64, 65}, chains
+
+
 def test_outputs_past_the_caches(tmp_path):
     """bf16 outputs of a tile per workgroup always, their 8-bit rows never (some wavefronts write 32 bytes of a row, and the next product reads all of
     it), large tiles' from 150 MB on; nothing whose rows do not start at multiples of 64 bytes."""
