@@ -18,8 +18,6 @@ namespace pab {
 typedef __attribute__((ext_vector_type(2))) unsigned u32x2;
 typedef __attribute__((ext_vector_type(4))) unsigned u32x4;
 
-constexpr int Q8_BLOCK = 128;
-
 // bits of |x|, 0 where x is not finite
 __device__ __forceinline__ unsigned finite_bits(float x) {
   const unsigned a = __float_as_uint(x) & 0x7fffffffu;
