@@ -4,7 +4,7 @@
 // What bounds it: the way of the weights from memory to the registers, once.  Nothing is shared between wavefronts but the sums, so operands
 // go from memory straight into the instruction's layout (16 rows of 64 bytes per load), those of three slices at a time requested before
 // the first product, and there is no LDS stage and no barrier in the K loop.  The sums are added through LDS, group by group in order.
-// 1 x 6912 x 1152 (8 MB of weights): 3.9 us with its launch, 5.1 with 64 x 64 tiles and K groups; 3 x 3256 x 4440 5.8, 9.9.  Slices deeper than three ahead
+// 1 x 6912 x 1152 (8 MB of weights): 4.1 us, 5.6 with 64 x 64 tiles and K groups; 3 x 3256 x 4440 5.9, 10.4.  Slices deeper than three ahead
 // change nothing.
 #pragma once
 #include "gemm_q8.hpp"

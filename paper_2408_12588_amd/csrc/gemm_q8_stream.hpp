@@ -17,13 +17,15 @@
 // the caches (q8_plan.hpp says when): what all workgroups of an XCD store at once is as large as its L2, and drives out the operands.  The 32-byte
 // pieces of odd sub-tiles never are: memory would read what it keeps of them (288-feature tiles, 53536 x 3584 x 200: 92 -> 135).
 //
-// Measured, us: a slice of 256 x 256 x 128 takes 1.58, of 256 x 288 1.70, and a tile 3 (8-bit or large outputs) to 5 and 8 more, with GELU 3 more.
-// With all operands in L2 a slice takes 1.37, without the copies 1.08, and the products alone, from registers, 0.9 to 1.0 (the clock
-// falls under them: random values 3.6 to 4.1 PF, zeros 4.9).  So the way from L2 into LDS bounds the loop, and what could be done about
-// its time was: two copies per step (all at once 2.12; in the second half 1.8; one or three per step slower), 128-byte rows, tile orders
-// that share operands within an XCD (groups of 2 to 16 token tiles: the same).  Four wavefronts of 128 x 128 with 512 registers run the loop as
-// fast and leave a tile more slowly; touching the slice after next for L2 gains 3 % at K = 1152 and loses 9 % at 4608.  Whole
-// products: 25440 x 3456 x 1152 98 (2.07 PF), 57600 x 1152 x 4608 273 (2.24 PF), 16384 x 4096 x 1152 into 8-bit rows 70 (2.2 PF), with GELU 83.
+// Measured, us: a slice of 256 x 256 x 128 takes 1.53 to 1.57 (1024 tiles, 9 to 36 slices deep), of 256 x 288 1.65 to 1.78, and a tile 3 (8-bit or
+// large outputs) to 6 and 8 more, with GELU 3 to 4 more.  The products of a slice alone, from registers, take 1.22 on random values, where power holds them to
+// 3.5 PF, and 0.99 on zeros (4.3 PF); its 66 KB take 1.10 at the 60 GB/s that L2 gives a CU when all ask.  Neither bounds the loop by itself: it takes
+// 1.37 with all operands in L2, 1.08 without the copies (the same values each time), and the barrier waits for every copy of a slice before the
+// first of the slice after next is sent, so that the way from L2 empties once in each.  Tried: two copies per step are best (all at
+// once 2.12; in the second half 1.8; one or three per step slower), tile orders that share operands within an XCD (groups of 2 to 16 token tiles) are
+// the same.  Four wavefronts of 128 x 128 with 512 registers run the loop as fast and leave a tile more slowly; touching the slice after next for
+// L2 gains 3 % at K = 1152 and loses 9 % at 4608.  Not tried: token copies that stay in flight across the barrier.  Whole products: 25440 x 3456 x
+// 1152 98 (2.06 PF), 57600 x 1152 x 4608 271 (2.26 PF), 16384 x 4096 x 1152 into 8-bit rows 73 (2.1 PF), with GELU 90.
 #pragma once
 #include "gemm_q8.hpp"
 

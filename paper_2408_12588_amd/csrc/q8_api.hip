@@ -158,8 +158,8 @@ int ln_modulate_q8(int n_tok, int C, const void *x, const void *shift, const voi
 
 // Workgroups of a long list of rows.  In bf16 a wavefront has as many values for half the bytes and is bound by its instructions: as many as the chip
 // holds at once (six per CU, 80 registers), which keep gamma and beta unpacked: 25440 tokens, 16 heads of 72, us at 1024 / 1536 / 2048 /
-// 4096 / one row group each: 56.3 / 50.0 / 59.8 / 54.2 / 65.5.  In fp32 nothing is unpacked and more, shorter ones are better: 12720 tokens 52.0 /
-// 51.6 / 52.3 / 49.9 / 49.1, at 8192 49.0.
+// 4096 / one row group each: 55.8 / 47.8 / 59.9 / 52.3 / 64.9.  In fp32 nothing is unpacked and more, shorter ones are better: 12720 tokens 51.5 /
+// 51.1 / 51.6 / 49.2 / 48.9, at 8192 48.9.
 template <typename T> constexpr long long QK_WGS = sizeof(T) == 2 ? 256 * 6 : 256 * 32;
 
 template <typename T, int NORM>

@@ -1,14 +1,16 @@
 // Which tiles a product of 8-bit rows takes: estimates as for the bf16 projections (launch_plan.hpp, with its kernel numbers), with constants of
 // their own, in us, at so many slices of 128.  A few tiles are bound by the latency of their K loop, more than one per CU by L2 and by their
 // stores.  Both sides of the lines, measured in us:
-//   16, 32, 48: gemm_q8_few for up to 16, 32, 64 tokens, against 64 x 64 tiles with K groups: 1 x 6912 x 1152 3.8 / 4.9, 3 x 3256 x 4440 5.7 / 9.9,
-//   17 x 1152 x 1152 3.5 / 4.9, 64 x 1152 x 1152 5.1 / 5.0, but 64 x 1152 x 4608 13.3 / 10.6, 20 x 4608 x 4608 13.5 / 10.4
+//   16, 32, 48: gemm_q8_few for up to 16, 32, 64 tokens, against 64 x 64 tiles with K groups, by kernel trace: 1 x 6912 x 1152 4.1 / 5.6, 3 x 3256 x 4440
+//   5.9 / 10.4, 17 x 1152 x 1152 4.0 / 5.4, 64 x 1152 x 1152 5.6 / 5.5, but 64 x 1152 x 4608 13.4 / 10.8, 20 x 4608 x 4608 13.6 / 10.7
 //   64 x 64 tiles, three K groups / one: 1 x 6912 x 1152 4.9 / 5.4, 1260 x 576 x 2304 7.4 / 8.5, but 1260 x 576 x 576 4.5 / 4.4
 //   96 x 128, two K groups / 128 x 128: 1260 x 2304 x 576 7.0 / 7.4, 2600 x 1152 x 4608 21.7 / 27.8
 //   160 x 128, two K groups / 128 x 128 / large tiles: 4413 x 1152 x 4608 27.3 / 31.3 / 41.7, 4413 x 1152 x 1152 10.5 / 11.4 / 15.5
 //   128 x 128 / large: 1260 x 3456 x 1152 11.1 / 14.5, 8000 x 1152 x 1152 18.9 / 18.4, 4413 x 4608 x 1152 33.5 / 30.2
 //   64 x 128 / 128 x 128, 8-bit outputs with GELU: 1260 x 1152 x 576 6.2 / 8.5, 1260 x 3456 x 1152 16.3 / 13.4
 //   large tiles, 256 / 288 features: 25440 x 3456 x 1152 98.8 / 99.2, 25440 x 1152 x 4608 128 / 133, 57600 x 1152 x 4608 294 / 273
+//   the same with GELU, whose 288-feature kernel spills three registers: where the plan takes 288, the choice without it / with it 8000 x 2304 x 4608 95 / 72,
+//   57600 x 1152 x 4608 308 / 288, but 25440 x 576 x 576 20.2 / 22.2; 10 % for it in the mean of 52 shapes
 // Against the best kernel of each of 1200 random shapes the choice loses 0.7 % in the mean.
 #pragma once
 #include <algorithm>

@@ -1,7 +1,9 @@
 // Passes over 8-bit rows (q8_common.hpp): values -> rows, layernorm + modulate -> rows, rows -> values with the gated residual.
-// Each touches every element once: large ones are bound by HBM, where a copy reaches 5.1 TB/s.  25440 rows of 1152, us: quantise bf16 (88 MB) 15.9,
-// read back with gate and residual (147 MB) 27.9, layernorm + modulate (88 MB) 22.1; layernorm of 2048 columns (156 MB) 29.3.  Looking at
-// each value for infinities by itself costs the quantisers a fifth (16.5, 24.8, 33.1): block_max looks at the largest only.
+// Each touches every element once: large ones are bound by memory.  25440 rows of 1152 / 2048, us, over four sets of buffers in turn: quantise bf16
+// (88 / 156 MB) 18.4 / 29.6, fp32 (147 / 261 MB) 26.5 / 45.6, read back with gate and residual (147 / 261 MB) 29.5 / 48.4: 4.8 to 5.7 TB/s where a copy of
+// 1 GiB reaches 5.1, because they read more than they write and find some of it in the last-level cache of 256 MB.  An output that takes the same
+// memory in every call stays there (quantise 14.9).  Layernorm + modulate, one set of buffers: 22.1 / 29.3.  Looking at each value for infinities by
+// itself costs 4, 12 and 13 % (quantise bf16 of 1152 columns 15.9 -> 16.5, layernorm 24.8, 33.1): block_max looks at the largest only.
 #pragma once
 #include "module_rowwise.hpp"
 #include "q8_common.hpp"

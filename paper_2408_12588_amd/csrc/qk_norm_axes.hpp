@@ -8,8 +8,8 @@
 // The table instead of angles computed here: it is (T dt + Y dy + X dx) / 2 pairs, a few KB that stay in L1, where the angle of a far place
 // needs fp64 to be right.  Bound by HBM, q and k read and written once.  LPR neighbouring lanes share a (token, head) row, 8 features each,
 // so that every load and store of a wavefront is one contiguous stretch; a lane has the same features of the same token's q and k,
-// whose factors it therefore loads once.  25440 tokens of 16 heads of 72 (234 MB): 50 us, 4.7 TB/s, where a copy reaches 5.1; with three lanes per
-// row, 24 features each, which read 16 bytes in every 48, 71 us; with one group of rows per wavefront, gamma and beta unpacked each time, 59.
+// whose factors it therefore loads once.  25440 tokens of 16 heads of 72 (234 MB): 48 us, 4.9 TB/s, where a copy reaches 5.1; with one group of rows per
+// wavefront, gamma and beta unpacked each time, 65; an earlier form with three lanes per row, 24 features each, which read 16 bytes in every 48, took 71.
 #pragma once
 #include "q8_common.hpp"
 #include "rope_table.hpp"
