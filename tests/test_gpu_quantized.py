@@ -271,6 +271,38 @@ def test_linear_scales_of_both_operands():
     assert np.all(np.abs(out.cpu().double().numpy() - want) <= tol)
 
 
+EXTREMES = [(8, 200, 384), (40, 256, 384), (300, 576, 1152), (1260, 1728, 576), (5000, 1152, 520)]
+
+
+@pytest.mark.parametrize("M,N,K", EXTREMES)
+def test_linear_scales_that_cancel(M, N, K):
+    """2^k in the tokens and 2^-k in the weights, as far as an exponent byte reaches, block by block another k: the bits of k = 0."""
+    a, b = make_q8(normal(23, M, K))[0], make_q8(normal(24, N, K) / K ** 0.5)[0]
+    want = pab.pab_linear_quantized(a, b)
+    nb = qo.blocks(K)
+    assert int(a.scale[:, :nb].max()) <= 127 - 6 and int(b.scale[:, :nb].min()) >= 127 - 14   # 448 * 2^-6 and 448 * 2^-14: magnitudes of the values
+    for k in (-113, -100, 100, 113):
+        step = torch.tensor([k if i % 2 == 0 else k // 2 for i in range(nb)], device=DEV)
+        sa, sb = a.scale.clone(), b.scale.clone()
+        sa[:, :nb] = (a.scale[:, :nb].int() + step).to(torch.uint8)
+        sb[:, :nb] = (b.scale[:, :nb].int() - step).to(torch.uint8)
+        got = pab.pab_linear_quantized(pab.Q8(a.data, sa, K), pab.Q8(b.data, sb, K))
+        assert torch.equal(got, want), k
+
+
+@pytest.mark.parametrize("M,N,K", EXTREMES)
+def test_linear_nan_scale_stays_in_its_row(M, N, K):
+    """An exponent byte of 255 makes its token's or its feature's sums NaN, and no others."""
+    a, b = make_q8(normal(25, M, K))[0], make_q8(normal(26, N, K) / K ** 0.5)[0]
+    want = pab.pab_linear_quantized(a, b)
+    sa, sb = a.scale.clone(), b.scale.clone()
+    sa[M // 2, qo.blocks(K) - 1], sb[N // 3, 0] = 255, 255
+    got = pab.pab_linear_quantized(pab.Q8(a.data, sa, K), pab.Q8(b.data, sb, K))
+    bad = torch.zeros(M, N, dtype=torch.bool, device=DEV)
+    bad[M // 2], bad[:, N // 3] = True, True
+    assert bool(got[bad].isnan().all()) and torch.equal(got[~bad], want[~bad])
+
+
 def test_linear_same_bits_twice_and_on_a_stream():
     a, b, bs, want, tol = check_product(1260, 1728, 576, True, True, 31)
     first = pab.pab_linear_quantized(a, b, bs, act=pab.GELU)
