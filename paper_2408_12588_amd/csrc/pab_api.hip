@@ -8,6 +8,7 @@
 #include <cstdint>
 #include <cstdio>
 #include <cstring>
+#include <memory>
 #include <new>
 #include <mutex>
 #include <vector>
@@ -328,22 +329,26 @@ int create_context(const pab_config *cfg, void *workspace, size_t workspace_byte
   if (!slot) return fail(PAB_EINVAL, "slots of 8-bit rows hold fewer than 2^28 blocks");
   if (workspace_bytes < need)
     return fail(PAB_ENOMEM, "workspace has %zu bytes, the cache needs %zu", workspace_bytes, need);
-  pab_ctx *ctx = new (std::nothrow) pab_ctx;
+  std::unique_ptr<pab_ctx> ctx(new (std::nothrow) pab_ctx);
   if (!ctx) return fail(PAB_ENOMEM, "out of host memory");
+  try {
+    ctx->slot_index.assign((size_t)cfg->n_blocks * 3, -1);
+    ctx->last_step.assign((size_t)cfg->n_blocks * 3, -1);
+    ctx->computed_step.assign((size_t)cfg->n_blocks * 3, -1);
+  } catch (const std::bad_alloc &) {
+    return fail(PAB_ENOMEM, "out of host memory");
+  }
   ctx->cfg = *cfg;
   ctx->workspace = static_cast<unsigned char *>(workspace);
   ctx->slot_bytes = slot;
   ctx->quantized = quantized;
-  ctx->slot_index.assign((size_t)cfg->n_blocks * 3, -1);
   long long next = 0;
   for (int b = 0; b < cfg->n_blocks; ++b)
     for (int k = 0; k < 3; ++k)
       if ((kinds_of_block(*cfg, b) >> k) & 1) ctx->slot_index[(size_t)b * 3 + k] = next++;
   ctx->cfg.block_kinds = nullptr;   // the caller's array is not kept
-  ctx->last_step.assign((size_t)cfg->n_blocks * 3, -1);
-  ctx->computed_step.assign((size_t)cfg->n_blocks * 3, -1);
   ctx->launches = 0;
-  *out = ctx;
+  *out = ctx.release();
   return PAB_OK;
 }
 
@@ -739,16 +744,20 @@ int pab_mlp_create(const pab_mlp_config *c, const int *start_steps, void *worksp
     if (reinterpret_cast<uintptr_t>(workspace) & 255u) return fail(PAB_EINVAL, "workspace must be 256-byte aligned");
     if (workspace_bytes < need) return fail(PAB_ENOMEM, "workspace of %zu bytes, need %zu", workspace_bytes, need);
   }
-  pab_mlp_ctx *ctx = new (std::nothrow) pab_mlp_ctx;
+  std::unique_ptr<pab_mlp_ctx> ctx(new (std::nothrow) pab_mlp_ctx);
   if (!ctx) return fail(PAB_ENOMEM, "out of host memory");
+  try {
+    ctx->starts.assign(start_steps, start_steps + c->n_starts);
+    ctx->last_step.assign(c->n_blocks, -1);
+    ctx->computed_step.assign(c->n_blocks, -1);
+  } catch (const std::bad_alloc &) {
+    return fail(PAB_ENOMEM, "out of host memory");
+  }
   ctx->cfg = *c;
-  ctx->starts.assign(start_steps, start_steps + c->n_starts);
   ctx->workspace = static_cast<unsigned char *>(workspace);
   ctx->slot_bytes = ((size_t)c->n_tok * c->hidden * 2 + 255) / 256 * 256;
-  ctx->last_step.assign(c->n_blocks, -1);
-  ctx->computed_step.assign(c->n_blocks, -1);
   ctx->launches = 0;
-  *out = ctx;
+  *out = ctx.release();
   return PAB_OK;
 }
 

@@ -1,6 +1,8 @@
 """Refusals and host logic of the 8-bit rows and of the query / key norm; nothing here reaches a GPU: every call fails its checks
 before a launch, and the pointers are numbers that nobody follows."""
 import ctypes
+import subprocess
+import sys
 
 import pytest
 
@@ -176,6 +178,37 @@ def test_quantized_slots_are_what_a_launch_fills():
     assert need == pab.pab_quantized_bytes(2**28 - 2**14, 128)
     assert status("pab_create_quantized", ctypes.byref(fits), OK, need, ctypes.byref(h)) == pab.OK
     pab.lib.pab_destroy(h)
+
+
+OUT_OF_MEMORY = """
+import ctypes, resource, sys
+lib = ctypes.CDLL(sys.argv[1])
+class Config(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int) for n in ("n_blocks", "T", "S", "L", "heads", "head_dim", "dtype", "n_steps")] + [
+        ("interval", ctypes.c_int * 3), ("range_lo", ctypes.c_int), ("range_hi", ctypes.c_int), ("block_kinds", ctypes.c_void_p)]
+used = int(open("/proc/self/statm").read().split()[0]) * resource.getpagesize()
+resource.setrlimit(resource.RLIMIT_AS, (used + (1 << 30),) * 2)
+cfg = Config(2**31 - 1, 1, 1, 0, 4, 32, 0, 4, (2, 0, 0), 0, 3, None)
+out = ctypes.c_void_p()
+for name in ("pab_create", "pab_create_quantized"):
+    f = getattr(lib, name)
+    f.argtypes = [ctypes.c_void_p, ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p]
+    assert f(ctypes.byref(cfg), 1 << 20, 1 << 62, ctypes.byref(out)) == -3 and not out.value, name
+class MlpConfig(ctypes.Structure):
+    _fields_ = [("n_blocks", ctypes.c_int), ("n_steps", ctypes.c_int), ("n_tok", ctypes.c_longlong)] + [
+        (n, ctypes.c_int) for n in ("hidden", "inner", "n_starts", "range", "block_lo", "block_hi")]
+cfg, start = MlpConfig(2**31 - 1, 4, 8, 32, 32, 1, 2, 0, 1), ctypes.c_int(1)
+lib.pab_mlp_create.argtypes = [ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p]
+assert lib.pab_mlp_create(ctypes.byref(cfg), ctypes.byref(start), 1 << 20, 1 << 62, ctypes.byref(out)) == -3 and not out.value
+"""
+
+
+def test_contexts_without_host_memory(tmp_path):
+    """More blocks than the host has memory for are an error, no exception through the C boundary (which would end the process)."""
+    script = tmp_path / "oom.py"
+    script.write_text(OUT_OF_MEMORY)
+    done = subprocess.run([sys.executable, str(script), pab.LIB_PATH], capture_output=True, text=True, timeout=120)
+    assert done.returncode == 0, done.stderr[-2000:]
 
 
 def test_quantized_context_refuses():
